@@ -21,8 +21,8 @@
  *     any alignment, the library aligns internally).
  *   - `stream` is a hipStream_t passed as void* (NULL = the null stream).
  *     All device work is enqueued on it.
- *   - ezsp_knn, ezsp_component_stats and ezsp_embed_mlp are
- *     stream-asynchronous: they validate their arguments, enqueue their
+ *   - ezsp_knn, ezsp_component_stats, ezsp_embed_mlp and the dense operators
+ *     (ezsp_layer_norm and after) are stream-asynchronous: they validate their arguments, enqueue their
  *     kernels and return; their outputs are ready once `stream` reaches
  *     that point, and their workspace must stay allocated until then.
  *     Errors the device detects (a non-finite coordinate, a label out of
@@ -295,6 +295,75 @@ int ezsp_embed_mlp(const uint16_t *x, int64_t n, int32_t d_in, int32_t d_hid,
                    const uint16_t *w2, const float *b2, const uint16_t *w3,
                    const float *b3, float *out, void *stream);
 
+/* ---- dense operators of a trainable embedding network (the point embedding
+ * of Sec. 3.1 is a network trained with the edge loss): layer norm, product
+ * with bias, activation and residual, gated feed-forward product, each with
+ * its backward pass ------------------------------------------------------- */
+
+/* Element types of the activations and weights below.  Biases, norm weights,
+ * their gradients and row statistics are fp32 with either. */
+#define EZSP_TYPE_BF16 0
+#define EZSP_TYPE_F32 1
+
+/* Activations: z, max(z, 0), z Phi(z) (Phi the normal distribution
+ * function), z / (1 + exp(-z)). */
+#define EZSP_ACT_NONE 0
+#define EZSP_ACT_RELU 1
+#define EZSP_ACT_GELU 2
+#define EZSP_ACT_SILU 3
+
+/* Conventions of this group
+ *   - A matrix of n rows is row-major with the distance between two rows
+ *     given in elements (ld*, at least the row's length), so that columns of
+ *     a wider table can be passed.  Weights are contiguous, [d_in][d_out].
+ *     Any alignment of an element is accepted; 16-byte aligned rows and
+ *     lengths that are multiples of 8 (bfloat16) or 4 (fp32) are fastest.
+ *   - Products and sums accumulate in fp32, whatever the element type; every
+ *     result is rounded once when it is stored, to nearest even.
+ *   - All calls are stream-asynchronous and the device detects no errors:
+ *     infinities and NaN follow IEEE arithmetic into the elements that
+ *     depend on them and no others.  (-inf gives NaN through SiLU and GELU,
+ *     as their formulas do.)
+ *   - Results are the same in every run: no sum depends on the order in
+ *     which blocks run.
+ *   - Outputs must not overlap inputs, except where noted.
+ *   - n in 1..2^31 - 256. */
+
+/* y = (x - mean) * rstd * weight + bias over each row of d values, with
+ * mean = sum(x) / d and rstd = 1 / sqrt(sum((x - mean)^2) / d + eps).
+ *   x       n rows of d, type_x (in); d in 1..16384
+ *   weight  d fp32 (in, nullable: 1); bias d fp32 (in, nullable: 0)
+ *   eps     finite and >= 0
+ *   y       n rows of d, type_y (out); may be x when the types and row
+ *           distances are the same
+ *   mean, rstd  n fp32 each (out, nullable)
+ * Errors: INVALID_ARG, DEVICE (the launch failed). */
+int ezsp_layer_norm(const void *x, int64_t ldx, int32_t type_x, int64_t n,
+                    int32_t d, const float *weight, const float *bias,
+                    double eps, void *y, int64_t ldy, int32_t type_y,
+                    float *mean, float *rstd, void *stream);
+
+size_t ezsp_layer_norm_backward_workspace_size(int64_t n, int32_t d);
+
+/* Gradients of ezsp_layer_norm.  With xh = (x - mean) * rstd and
+ * g = dy * weight over each row:
+ *   dx = (g - sum(g)/d - xh * sum(g * xh)/d) * rstd (+ dres)
+ *   dweight = sum over rows of dy * xh,  dbias = sum over rows of dy
+ *   dy      n rows of d, type_y (in)
+ *   x       n rows of d, type_x (in); mean, rstd n fp32 (in)
+ *   dres    n rows of d, type_x (in, nullable): a gradient that reaches x
+ *           past the norm (a residual branch), added to dx
+ *   dx      n rows of d, type_x (out, nullable); may be dres
+ *   dweight, dbias  d fp32 (out, each nullable)
+ * Errors: INVALID_ARG, WORKSPACE, DEVICE. */
+int ezsp_layer_norm_backward(const void *dy, int64_t lddy, int32_t type_y,
+                             const void *x, int64_t ldx, int32_t type_x,
+                             int64_t n, int32_t d, const float *weight,
+                             const float *mean, const float *rstd,
+                             const void *dres, int64_t lddres, void *dx,
+                             int64_t lddx, float *dweight, float *dbias,
+                             void *ws, size_t ws_bytes, void *stream);
+
 /* ---- kNN without a workspace --------------------------------------------- */
 
 /* For callers that cannot allocate device memory (code under HIP graph
@@ -331,7 +400,7 @@ const char *ezsp_last_error(void);
 /* Per-stage timing with HIP events recorded on the caller's stream around
  * the launches of each stage ("knn_query", "morton_sort", "graph_build",
  * "select", "union", "stats", "contract", "compose", "tail", "link",
- * "grid_subsample", "edge_loss", "purity", "embed_mlp").  Off by default; a
+ * "grid_subsample", "edge_loss", "purity", "embed_mlp", "layer_norm").  Off by default; a
  * diagnostic for benchmarks.  ezsp_profile_enable(1) clears the totals and
  * starts recording, ezsp_profile_enable(0) stops.  ezsp_profile_read gives
  * the number of recorded launches of `stage`, their summed duration in

@@ -46,6 +46,8 @@ bool edges_ok(int64_t n, int32_t k) {
   return 4 * n * (int64_t)k < kMaxN - 1;
 }
 
+bool type_ok(int32_t t) { return t == EZSP_TYPE_BF16 || t == EZSP_TYPE_F32; }
+
 int check_params(int64_t n, int32_t d, const ezsp_params *p) {
   if (!p) return fail(EZSP_ERR_INVALID_ARG, "params is NULL");
   if (!n_ok(n)) return fail(EZSP_ERR_INVALID_ARG, "n must be in [1, 2^31 - 256]");
@@ -447,6 +449,94 @@ int ezsp_embed_mlp(const uint16_t *x, int64_t n, int32_t d_in, int32_t d_hid,
     return fail(EZSP_ERR_INVALID_ARG, "n*d_out must stay below 2^31");
   return mlp_run(x, (int32_t)n, d_in, d_out, w1, b1, w2, b2, w3, b3, out,
                  static_cast<hipStream_t>(stream));
+}
+
+int ezsp_layer_norm(const void *x, int64_t ldx, int32_t type_x, int64_t n,
+                    int32_t d, const float *weight, const float *bias,
+                    double eps, void *y, int64_t ldy, int32_t type_y,
+                    float *mean, float *rstd, void *stream) {
+  set_error("%s", "");
+  if (!x || !y) return fail(EZSP_ERR_INVALID_ARG, "x and y must not be NULL");
+  if (!n_ok(n)) return fail(EZSP_ERR_INVALID_ARG, "n must be in [1, 2^31 - 256]");
+  if (d < 1 || d > kNormMaxD)
+    return fail(EZSP_ERR_INVALID_ARG, "d must be in 1..16384");
+  if (!type_ok(type_x) || !type_ok(type_y))
+    return fail(EZSP_ERR_INVALID_ARG, "unknown element type");
+  if (ldx < d || ldy < d)
+    return fail(EZSP_ERR_INVALID_ARG, "row distances must be at least d");
+  if (!(eps >= 0.0) || !isfinite(eps))
+    return fail(EZSP_ERR_INVALID_ARG, "eps must be finite and >= 0");
+  NormArgs a;
+  memset(&a, 0, sizeof(a));
+  a.x = x;
+  a.ldx = ldx;
+  a.type_x = type_x;
+  a.type_y = type_y;
+  a.n = n;
+  a.d = d;
+  a.w = weight;
+  a.b = bias;
+  a.eps = eps;
+  a.y = y;
+  a.ldy = ldy;
+  a.mean = mean;
+  a.rstd = rstd;
+  return norm_fwd_run(a, static_cast<hipStream_t>(stream));
+}
+
+size_t ezsp_layer_norm_backward_workspace_size(int64_t n, int32_t d) {
+  if (!n_ok(n) || d < 1 || d > kNormMaxD) return 0;
+  return (size_t)(n < kNormParts ? n : kNormParts) * 2 * (size_t)d *
+             sizeof(float) + 512;
+}
+
+int ezsp_layer_norm_backward(const void *dy, int64_t lddy, int32_t type_y,
+                             const void *x, int64_t ldx, int32_t type_x,
+                             int64_t n, int32_t d, const float *weight,
+                             const float *mean, const float *rstd,
+                             const void *dres, int64_t lddres, void *dx,
+                             int64_t lddx, float *dweight, float *dbias,
+                             void *ws, size_t ws_bytes, void *stream) {
+  set_error("%s", "");
+  if (!dy || !x || !mean || !rstd || !ws)
+    return fail(EZSP_ERR_INVALID_ARG,
+                "dy, x, mean, rstd and ws must not be NULL");
+  if (!dx && !dweight && !dbias)
+    return fail(EZSP_ERR_INVALID_ARG, "no gradient is asked for");
+  if (dres && !dx)
+    return fail(EZSP_ERR_INVALID_ARG, "dres is added to dx: dx is NULL");
+  if (!n_ok(n)) return fail(EZSP_ERR_INVALID_ARG, "n must be in [1, 2^31 - 256]");
+  if (d < 1 || d > kNormMaxD)
+    return fail(EZSP_ERR_INVALID_ARG, "d must be in 1..16384");
+  if (!type_ok(type_x) || !type_ok(type_y))
+    return fail(EZSP_ERR_INVALID_ARG, "unknown element type");
+  if (ldx < d || lddy < d || (dx && lddx < d) || (dres && lddres < d))
+    return fail(EZSP_ERR_INVALID_ARG, "row distances must be at least d");
+  if (ws_bytes < ezsp_layer_norm_backward_workspace_size(n, d))
+    return fail(EZSP_ERR_WORKSPACE, "workspace smaller than the queried size");
+  NormArgs a;
+  memset(&a, 0, sizeof(a));
+  a.x = x;
+  a.ldx = ldx;
+  a.type_x = type_x;
+  a.type_y = type_y;
+  a.n = n;
+  a.d = d;
+  a.w = weight;
+  a.mean = const_cast<float *>(mean);
+  a.rstd = const_cast<float *>(rstd);
+  a.dy = dy;
+  a.lddy = lddy;
+  a.dres = dres;
+  a.lddres = lddres;
+  a.dx = dx;
+  a.lddx = lddx;
+  a.dw = dweight;
+  a.db = dbias;
+  Arena ar = open_ws(ws, ws_bytes);
+  a.part = ar.take<float>((size_t)(n < kNormParts ? n : kNormParts) * 2 *
+                          (size_t)d);
+  return norm_bwd_run(a, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

@@ -231,6 +231,32 @@ int mlp_run(const uint16_t *x, int32_t n, int32_t d_in, int32_t d_out,
             const float *b2, const uint16_t *w3, const float *b3, float *out,
             hipStream_t st);
 
+// Layer norm, forward and backward (types are EZSP_TYPE_*).
+struct NormArgs {
+  const void *x;
+  int64_t ldx;
+  int32_t type_x, type_y;
+  int64_t n;
+  int32_t d;
+  const float *w, *b;     // nullable
+  double eps;
+  void *y;                // forward
+  int64_t ldy;
+  float *mean, *rstd;     // forward: out, nullable; backward: in
+  const void *dy;         // backward
+  int64_t lddy;
+  const void *dres;       // nullable
+  int64_t lddres;
+  void *dx;               // nullable
+  int64_t lddx;
+  float *dw, *db;         // nullable
+  float *part;            // kNormParts * 2 * d
+};
+constexpr int32_t kNormMaxD = 16384;
+constexpr int32_t kNormParts = 1024;
+int norm_fwd_run(const NormArgs &a, hipStream_t st);
+int norm_bwd_run(const NormArgs &a, hipStream_t st);
+
 // Shared host helpers.
 void set_error(const char *fmt, ...);
 int read_ctl(Ctl *ctl, Ctl *host, hipStream_t st);  // sync + copy back

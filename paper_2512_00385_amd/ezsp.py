@@ -39,6 +39,8 @@ ENTRY_POINTS = (
     "ezsp_purity_workspace_size", "ezsp_purity",
     "ezsp_embed_mlp", "ezsp_sync_status", "ezsp_knn_noalloc",
     "ezsp_knn_walk_stats",
+    "ezsp_layer_norm", "ezsp_layer_norm_backward_workspace_size",
+    "ezsp_layer_norm_backward",
 )
 
 
@@ -115,6 +117,13 @@ def load() -> ctypes.CDLL:
         "ezsp_knn_noalloc": (ctypes.c_int, [P, i64, i32, P, P, P]),
         "ezsp_knn_walk_stats": (ctypes.c_int, [P, i64, i32, P, P, P, P, sz,
                                                P]),
+        "ezsp_layer_norm": (ctypes.c_int, [P, i64, i32, i64, i32, P, P,
+                                           ctypes.c_double, P, i64, i32, P,
+                                           P, P]),
+        "ezsp_layer_norm_backward_workspace_size": (sz, [i64, i32]),
+        "ezsp_layer_norm_backward": (ctypes.c_int, [
+            P, i64, i32, P, i64, i32, i64, i32, P, P, P, P, i64, P, i64, P, P,
+            P, sz, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -144,7 +153,8 @@ def profile_only(stage=None):
 
 STAGES = ("morton_sort", "knn_query", "graph_build", "select", "union",
           "stats", "contract", "compose", "tail", "link")
-EXTRA_STAGES = ("grid_subsample", "edge_loss", "purity", "embed_mlp")
+EXTRA_STAGES = ("grid_subsample", "edge_loss", "purity", "embed_mlp",
+                "layer_norm")
 
 
 def profile_read(stage: str):
@@ -480,3 +490,106 @@ def embed_mlp(x_bits: torch.Tensor, w1, b1, w2, b2, w3, b3) -> torch.Tensor:
                               _ptr(b3), _ptr(out), _stream(x.device)),
            "ezsp_embed_mlp")
     return out
+
+
+# ---- dense operators of a trainable embedding network ---------------------
+
+TYPE_CODES = {torch.bfloat16: 0, torch.float32: 1}
+ACT_CODES = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
+
+
+def _rows(t, name, like=None, cols=None, dtype=None):
+    """A [n, d] device tensor whose rows are contiguous (columns of a wider
+    table stay as they are, other orders are copied) and the distance
+    between its rows."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a device tensor")
+    if dtype is not None and t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dtype not in TYPE_CODES:
+        raise TypeError(f"{name} must be bfloat16 or float32, got {t.dtype}")
+    if t.dim() != 2:
+        raise ValueError(f"{name} must have shape [n, d]")
+    n, d = t.shape
+    if like is not None and (n != like or d != cols):
+        raise ValueError(f"{name} must have shape [{like}, {cols}], got "
+                         f"{list(t.shape)}")
+    ld, one = t.stride()
+    if (one != 1 and d > 1) or (ld < d and n > 1):
+        t = t.contiguous()
+        ld = d
+    return t, max(ld, d)
+
+
+def _vector(t, d, name):
+    """A contiguous fp32 device vector of d values, or None."""
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a device tensor")
+    if t.dtype != torch.float32:
+        raise TypeError(f"{name} must be torch.float32, got {t.dtype}")
+    if t.shape != (d,):
+        raise ValueError(f"{name} must have shape [{d}]")
+    return t.contiguous()
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
+
+
+def layer_norm(x: torch.Tensor, weight=None, bias=None, eps: float = 1e-5,
+               out_dtype=None, want_stats: bool = False):
+    """Layer norm over each row of x [n, d] (ezsp_layer_norm), bfloat16 or
+    fp32, weight and bias [d] fp32 or None; y has out_dtype (x's by
+    default).  Returns y, or with want_stats (y, mean [n], rstd [n]) for
+    layer_norm_backward.  Computed in stream order."""
+    lib = load()
+    x, ldx = _rows(x, "x")
+    n, d = x.shape
+    weight, bias = _vector(weight, d, "weight"), _vector(bias, d, "bias")
+    out_dtype = out_dtype or x.dtype
+    if out_dtype not in TYPE_CODES:
+        raise TypeError("out_dtype must be bfloat16 or float32")
+    y = torch.empty((n, d), dtype=out_dtype, device=x.device)
+    mean = rstd = None
+    if want_stats:
+        mean = torch.empty(n, dtype=torch.float32, device=x.device)
+        rstd = torch.empty(n, dtype=torch.float32, device=x.device)
+    _check(lib.ezsp_layer_norm(
+        x.data_ptr(), ldx, TYPE_CODES[x.dtype], n, d, _at(weight), _at(bias),
+        float(eps), y.data_ptr(), d, TYPE_CODES[out_dtype], _at(mean),
+        _at(rstd), _stream(x.device)), "ezsp_layer_norm")
+    return (y, mean, rstd) if want_stats else y
+
+
+def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor,
+                        mean: torch.Tensor, rstd: torch.Tensor, weight=None,
+                        dres=None, want_dx: bool = True,
+                        want_sums: bool = True):
+    """Gradients of layer_norm (ezsp_layer_norm_backward): (dx [n, d] of x's
+    type, dweight [d], dbias [d] fp32), each None where it is not wanted.
+    dres [n, d], of x's type, is added to dx."""
+    lib = load()
+    x, ldx = _rows(x, "x")
+    n, d = x.shape
+    dy, lddy = _rows(dy, "dy", n, d)
+    mean, rstd = _vector(mean, n, "mean"), _vector(rstd, n, "rstd")
+    weight = _vector(weight, d, "weight")
+    lddres = 0
+    if dres is not None:
+        dres, lddres = _rows(dres, "dres", n, d, x.dtype)
+    dev = x.device
+    dx = torch.empty((n, d), dtype=x.dtype, device=dev) if want_dx else None
+    dw = db = None
+    if want_sums:
+        dw = torch.empty(d, dtype=torch.float32, device=dev)
+        db = torch.empty(d, dtype=torch.float32, device=dev)
+    nbytes = lib.ezsp_layer_norm_backward_workspace_size(n, d)
+    ws = _workspace(nbytes, dev)
+    _check(lib.ezsp_layer_norm_backward(
+        dy.data_ptr(), lddy, TYPE_CODES[dy.dtype], x.data_ptr(), ldx,
+        TYPE_CODES[x.dtype], n, d, _at(weight), _at(mean), _at(rstd),
+        _at(dres), lddres, _at(dx), d, _at(dw), _at(db), ws.data_ptr(),
+        nbytes, _stream(dev)), "ezsp_layer_norm_backward")
+    return dx, dw, db
