@@ -364,6 +364,85 @@ int ezsp_layer_norm_backward(const void *dy, int64_t lddy, int32_t type_y,
                              int64_t lddx, float *dweight, float *dbias,
                              void *ws, size_t ws_bytes, void *stream);
 
+size_t ezsp_linear_workspace_size(int64_t n, int32_t d_in, int32_t d_out);
+
+/* z = x w + bias, y = act(z) + residual.
+ *   x         n rows of d_in, type (in); d_in, d_out in 1..65536
+ *   w         d_in*d_out, type (in)
+ *   bias      d_out fp32 (in, nullable)
+ *   residual  n rows of d_out, type_y (in, nullable)
+ *   y         n rows of d_out, type_y (out); may be residual.  type_y is
+ *             type, or fp32 with bfloat16 inputs
+ *   z         n rows of d_out, type (out, nullable): what the backward pass
+ *             of an activation reads
+ * Errors: INVALID_ARG, WORKSPACE, DEVICE. */
+int ezsp_linear(const void *x, int64_t ldx, int64_t n, int32_t d_in,
+                int32_t d_out, int32_t type, const void *w, const float *bias,
+                int32_t act, const void *residual, int64_t ldr, void *y,
+                int64_t ldy, int32_t type_y, void *z, int64_t ldz, void *ws,
+                size_t ws_bytes, void *stream);
+
+size_t ezsp_linear_backward_workspace_size(int64_t n, int32_t d_in,
+                                           int32_t d_out, int32_t type);
+
+/* Gradients of ezsp_linear with respect to x, w and bias (the residual's is
+ * dy): dz = dy * act'(z), dx = dz w^T, dw = x^T dz, dbias = sum over rows of
+ * dz.  ReLU's derivative at 0 is 0.
+ *   dy     n rows of d_out, type_y (in)
+ *   z      n rows of d_out, type (in; NULL with EZSP_ACT_NONE)
+ *   dx     n rows of d_in, type (out, nullable)
+ *   dw     d_in*d_out, type (out, nullable)
+ *   dbias  d_out fp32 (out, nullable)
+ * With bfloat16, dx and dw take dz rounded to bfloat16 (the matrix cores'
+ * input); dbias sums it unrounded.
+ * Errors: INVALID_ARG, WORKSPACE, DEVICE. */
+int ezsp_linear_backward(const void *dy, int64_t lddy, int32_t type_y,
+                         const void *x, int64_t ldx, int64_t n, int32_t d_in,
+                         int32_t d_out, int32_t type, const void *w,
+                         const void *z, int64_t ldz, int32_t act, void *dx,
+                         int64_t lddx, void *dw, float *dbias, void *ws,
+                         size_t ws_bytes, void *stream);
+
+size_t ezsp_gated_ff_workspace_size(int64_t n, int32_t d_in, int32_t d_out);
+
+/* gate = x w_gate + b_gate, up = x w_up + b_up, h = act(gate) * up, both
+ * products, the activation and their product in one kernel.
+ *   x             n rows of d_in, type (in); d_in, d_out in 1..65536
+ *   w_gate, w_up  d_in*d_out each, type (in)
+ *   b_gate, b_up  d_out fp32 each (in, each nullable)
+ *   h             n rows of d_out, type (out)
+ *   gate, up      n rows of d_out, type, both with row distance lds (out,
+ *                 each nullable): what the backward pass reads
+ * Errors: INVALID_ARG, WORKSPACE, DEVICE. */
+int ezsp_gated_ff(const void *x, int64_t ldx, int64_t n, int32_t d_in,
+                  int32_t d_out, int32_t type, const void *w_gate,
+                  const float *b_gate, const void *w_up, const float *b_up,
+                  int32_t act, void *h, int64_t ldh, void *gate, void *up,
+                  int64_t lds, void *ws, size_t ws_bytes, void *stream);
+
+size_t ezsp_gated_ff_backward_workspace_size(int64_t n, int32_t d_in,
+                                             int32_t d_out, int32_t type);
+
+/* Gradients of ezsp_gated_ff: dgate = dh * up * act'(gate),
+ * dup = dh * act(gate), dx = dgate w_gate^T + dup w_up^T,
+ * dw_gate = x^T dgate, dw_up = x^T dup, and the row sums of dgate and dup.
+ *   dh, gate, up    n rows of d_out, type (in; gate and up with distance
+ *                   lds)
+ *   dx              n rows of d_in, type (out, nullable)
+ *   dw_gate, dw_up  d_in*d_out each, type (out, each nullable)
+ *   db_gate, db_up  d_out fp32 each (out, each nullable)
+ * With bfloat16, the products take dgate and dup rounded to bfloat16; the
+ * row sums take them unrounded.
+ * Errors: INVALID_ARG, WORKSPACE, DEVICE. */
+int ezsp_gated_ff_backward(const void *dh, int64_t lddh, const void *x,
+                           int64_t ldx, int64_t n, int32_t d_in,
+                           int32_t d_out, int32_t type, const void *w_gate,
+                           const void *w_up, const void *gate, const void *up,
+                           int64_t lds, int32_t act, void *dx, int64_t lddx,
+                           void *dw_gate, void *dw_up, float *db_gate,
+                           float *db_up, void *ws, size_t ws_bytes,
+                           void *stream);
+
 /* ---- kNN without a workspace --------------------------------------------- */
 
 /* For callers that cannot allocate device memory (code under HIP graph
@@ -400,8 +479,8 @@ const char *ezsp_last_error(void);
 /* Per-stage timing with HIP events recorded on the caller's stream around
  * the launches of each stage ("knn_query", "morton_sort", "graph_build",
  * "select", "union", "stats", "contract", "compose", "tail", "link",
- * "grid_subsample", "edge_loss", "purity", "embed_mlp", "layer_norm").  Off by default; a
- * diagnostic for benchmarks.  ezsp_profile_enable(1) clears the totals and
+ * "grid_subsample", "edge_loss", "purity", "embed_mlp", "layer_norm",
+ * "linear", "gated_ff").  Off by default; a diagnostic for benchmarks.  ezsp_profile_enable(1) clears the totals and
  * starts recording, ezsp_profile_enable(0) stops.  ezsp_profile_read gives
  * the number of recorded launches of `stage`, their summed duration in
  * milliseconds and the summed algorithmic bytes the stage has to move (its

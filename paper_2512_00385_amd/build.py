@@ -20,7 +20,7 @@ BUILD = os.path.join(HERE, "_build")
 SOURCES = ["ezsp_prims.hip", "ezsp_knn.hip", "ezsp_merge.hip",
            "ezsp_stats.hip", "ezsp_grid.hip", "ezsp_loss.hip",
            "ezsp_purity.hip", "ezsp_mlp.hip", "ezsp_noalloc.hip",
-           "ezsp_norm.hip",
+           "ezsp_norm.hip", "ezsp_linear.hip", "ezsp_gated.hip",
            "ezsp_api.hip"]
 ARCH = os.environ.get("EZSP_OFFLOAD_ARCH", "gfx950")
 

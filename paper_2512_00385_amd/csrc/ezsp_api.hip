@@ -48,6 +48,33 @@ bool edges_ok(int64_t n, int32_t k) {
 
 bool type_ok(int32_t t) { return t == EZSP_TYPE_BF16 || t == EZSP_TYPE_F32; }
 
+bool act_ok(int32_t a) { return a >= EZSP_ACT_NONE && a <= EZSP_ACT_SILU; }
+
+constexpr int32_t kMaxWidth = 65536;
+bool widths_ok(int32_t d_in, int32_t d_out) {
+  return d_in >= 1 && d_in <= kMaxWidth && d_out >= 1 && d_out <= kMaxWidth;
+}
+
+// What the products of the dense operators share.
+int check_product(int64_t n, int32_t d_in, int32_t d_out, int32_t type,
+                  int32_t act) {
+  if (!n_ok(n)) return fail(EZSP_ERR_INVALID_ARG, "n must be in [1, 2^31 - 256]");
+  if (!widths_ok(d_in, d_out))
+    return fail(EZSP_ERR_INVALID_ARG, "d_in and d_out must be in 1..65536");
+  if (!type_ok(type))
+    return fail(EZSP_ERR_INVALID_ARG, "unknown element type");
+  if (!act_ok(act)) return fail(EZSP_ERR_INVALID_ARG, "unknown activation");
+  return EZSP_OK;
+}
+
+// Bytes of a workspace that `reserve` fills.
+template <class F>
+size_t reserved(F reserve) {
+  Arena a;
+  reserve(a);
+  return a.off + 512;
+}
+
 int check_params(int64_t n, int32_t d, const ezsp_params *p) {
   if (!p) return fail(EZSP_ERR_INVALID_ARG, "params is NULL");
   if (!n_ok(n)) return fail(EZSP_ERR_INVALID_ARG, "n must be in [1, 2^31 - 256]");
@@ -537,6 +564,214 @@ int ezsp_layer_norm_backward(const void *dy, int64_t lddy, int32_t type_y,
   a.part = ar.take<float>((size_t)(n < kNormParts ? n : kNormParts) * 2 *
                           (size_t)d);
   return norm_bwd_run(a, static_cast<hipStream_t>(stream));
+}
+
+size_t ezsp_linear_workspace_size(int64_t n, int32_t d_in, int32_t d_out) {
+  if (!n_ok(n) || !widths_ok(d_in, d_out)) return 0;
+  return reserved([&](Arena &ar) {
+    LinearArgs a;
+    linear_reserve(ar, n, d_in, d_out, EZSP_TYPE_F32, false, &a);
+  });
+}
+
+int ezsp_linear(const void *x, int64_t ldx, int64_t n, int32_t d_in,
+                int32_t d_out, int32_t type, const void *w, const float *bias,
+                int32_t act, const void *residual, int64_t ldr, void *y,
+                int64_t ldy, int32_t type_y, void *z, int64_t ldz, void *ws,
+                size_t ws_bytes, void *stream) {
+  set_error("%s", "");
+  if (!x || !w || !y || !ws)
+    return fail(EZSP_ERR_INVALID_ARG, "x, w, y and ws must not be NULL");
+  const int rc = check_product(n, d_in, d_out, type, act);
+  if (rc) return rc;
+  if (type_y != type && type_y != EZSP_TYPE_F32)
+    return fail(EZSP_ERR_INVALID_ARG, "y has the inputs' type or fp32");
+  if (ldx < d_in || ldy < d_out || (residual && ldr < d_out) ||
+      (z && ldz < d_out))
+    return fail(EZSP_ERR_INVALID_ARG,
+                "row distances must be at least the rows' lengths");
+  if (ws_bytes < ezsp_linear_workspace_size(n, d_in, d_out))
+    return fail(EZSP_ERR_WORKSPACE, "workspace smaller than the queried size");
+  LinearArgs a;
+  memset(&a, 0, sizeof(a));
+  Arena ar = open_ws(ws, ws_bytes);
+  linear_reserve(ar, n, d_in, d_out, type, false, &a);
+  a.n = (int32_t)n;
+  a.d_in = d_in;
+  a.d_out = d_out;
+  a.type = type;
+  a.type_y = type_y;
+  a.act = act;
+  a.x = x;
+  a.ldx = ldx;
+  a.w = w;
+  a.bias = bias;
+  a.res = residual;
+  a.ldr = ldr;
+  a.y = y;
+  a.ldy = ldy;
+  a.z = z;
+  a.ldz = ldz;
+  return linear_fwd_run(a, static_cast<hipStream_t>(stream));
+}
+
+size_t ezsp_linear_backward_workspace_size(int64_t n, int32_t d_in,
+                                           int32_t d_out, int32_t type) {
+  if (!n_ok(n) || !widths_ok(d_in, d_out) || !type_ok(type)) return 0;
+  return reserved([&](Arena &ar) {
+    LinearArgs a;
+    linear_reserve(ar, n, d_in, d_out, type, true, &a);
+  });
+}
+
+int ezsp_linear_backward(const void *dy, int64_t lddy, int32_t type_y,
+                         const void *x, int64_t ldx, int64_t n, int32_t d_in,
+                         int32_t d_out, int32_t type, const void *w,
+                         const void *z, int64_t ldz, int32_t act, void *dx,
+                         int64_t lddx, void *dw, float *dbias, void *ws,
+                         size_t ws_bytes, void *stream) {
+  set_error("%s", "");
+  if (!dy || !x || !w || !ws)
+    return fail(EZSP_ERR_INVALID_ARG, "dy, x, w and ws must not be NULL");
+  if (!dx && !dw && !dbias)
+    return fail(EZSP_ERR_INVALID_ARG, "no gradient is asked for");
+  const int rc = check_product(n, d_in, d_out, type, act);
+  if (rc) return rc;
+  if (act != EZSP_ACT_NONE && !z)
+    return fail(EZSP_ERR_INVALID_ARG, "an activation's gradient needs z");
+  if (type_y != type && type_y != EZSP_TYPE_F32)
+    return fail(EZSP_ERR_INVALID_ARG, "dy has the inputs' type or fp32");
+  if (ldx < d_in || lddy < d_out || (z && ldz < d_out) || (dx && lddx < d_in))
+    return fail(EZSP_ERR_INVALID_ARG,
+                "row distances must be at least the rows' lengths");
+  if (ws_bytes < ezsp_linear_backward_workspace_size(n, d_in, d_out, type))
+    return fail(EZSP_ERR_WORKSPACE, "workspace smaller than the queried size");
+  LinearArgs a;
+  memset(&a, 0, sizeof(a));
+  Arena ar = open_ws(ws, ws_bytes);
+  linear_reserve(ar, n, d_in, d_out, type, true, &a);
+  a.n = (int32_t)n;
+  a.d_in = d_in;
+  a.d_out = d_out;
+  a.type = type;
+  a.type_y = type_y;
+  a.act = act;
+  a.x = x;
+  a.ldx = ldx;
+  a.w = w;
+  a.z = const_cast<void *>(z);
+  a.ldz = ldz;
+  a.dy = dy;
+  a.lddy = lddy;
+  a.dx = dx;
+  a.lddx = lddx;
+  a.dw = dw;
+  a.db = dbias;
+  return linear_bwd_run(a, static_cast<hipStream_t>(stream));
+}
+
+size_t ezsp_gated_ff_workspace_size(int64_t n, int32_t d_in, int32_t d_out) {
+  if (!n_ok(n) || !widths_ok(d_in, d_out)) return 0;
+  return reserved([&](Arena &ar) {
+    GatedArgs a;
+    gated_reserve(ar, n, d_in, d_out, EZSP_TYPE_F32, false, &a);
+  });
+}
+
+int ezsp_gated_ff(const void *x, int64_t ldx, int64_t n, int32_t d_in,
+                  int32_t d_out, int32_t type, const void *w_gate,
+                  const float *b_gate, const void *w_up, const float *b_up,
+                  int32_t act, void *h, int64_t ldh, void *gate, void *up,
+                  int64_t lds, void *ws, size_t ws_bytes, void *stream) {
+  set_error("%s", "");
+  if (!x || !w_gate || !w_up || !h || !ws)
+    return fail(EZSP_ERR_INVALID_ARG,
+                "x, w_gate, w_up, h and ws must not be NULL");
+  const int rc = check_product(n, d_in, d_out, type, act);
+  if (rc) return rc;
+  if (ldx < d_in || ldh < d_out || ((gate || up) && lds < d_out))
+    return fail(EZSP_ERR_INVALID_ARG,
+                "row distances must be at least the rows' lengths");
+  if (ws_bytes < ezsp_gated_ff_workspace_size(n, d_in, d_out))
+    return fail(EZSP_ERR_WORKSPACE, "workspace smaller than the queried size");
+  GatedArgs a;
+  memset(&a, 0, sizeof(a));
+  Arena ar = open_ws(ws, ws_bytes);
+  gated_reserve(ar, n, d_in, d_out, type, false, &a);
+  a.n = (int32_t)n;
+  a.d_in = d_in;
+  a.d_out = d_out;
+  a.type = type;
+  a.act = act;
+  a.x = x;
+  a.ldx = ldx;
+  a.w_gate = w_gate;
+  a.w_up = w_up;
+  a.b_gate = b_gate;
+  a.b_up = b_up;
+  a.h = h;
+  a.ldh = ldh;
+  a.gate = gate;
+  a.up = up;
+  a.lds = lds;
+  return gated_fwd_run(a, static_cast<hipStream_t>(stream));
+}
+
+size_t ezsp_gated_ff_backward_workspace_size(int64_t n, int32_t d_in,
+                                             int32_t d_out, int32_t type) {
+  if (!n_ok(n) || !widths_ok(d_in, d_out) || !type_ok(type)) return 0;
+  return reserved([&](Arena &ar) {
+    GatedArgs a;
+    gated_reserve(ar, n, d_in, d_out, type, true, &a);
+  });
+}
+
+int ezsp_gated_ff_backward(const void *dh, int64_t lddh, const void *x,
+                           int64_t ldx, int64_t n, int32_t d_in,
+                           int32_t d_out, int32_t type, const void *w_gate,
+                           const void *w_up, const void *gate, const void *up,
+                           int64_t lds, int32_t act, void *dx, int64_t lddx,
+                           void *dw_gate, void *dw_up, float *db_gate,
+                           float *db_up, void *ws, size_t ws_bytes,
+                           void *stream) {
+  set_error("%s", "");
+  if (!dh || !x || !w_gate || !w_up || !gate || !up || !ws)
+    return fail(EZSP_ERR_INVALID_ARG,
+                "dh, x, the weights, gate, up and ws must not be NULL");
+  if (!dx && !dw_gate && !dw_up && !db_gate && !db_up)
+    return fail(EZSP_ERR_INVALID_ARG, "no gradient is asked for");
+  const int rc = check_product(n, d_in, d_out, type, act);
+  if (rc) return rc;
+  if (ldx < d_in || lddh < d_out || lds < d_out || (dx && lddx < d_in))
+    return fail(EZSP_ERR_INVALID_ARG,
+                "row distances must be at least the rows' lengths");
+  if (ws_bytes < ezsp_gated_ff_backward_workspace_size(n, d_in, d_out, type))
+    return fail(EZSP_ERR_WORKSPACE, "workspace smaller than the queried size");
+  GatedArgs a;
+  memset(&a, 0, sizeof(a));
+  Arena ar = open_ws(ws, ws_bytes);
+  gated_reserve(ar, n, d_in, d_out, type, true, &a);
+  a.n = (int32_t)n;
+  a.d_in = d_in;
+  a.d_out = d_out;
+  a.type = type;
+  a.act = act;
+  a.x = x;
+  a.ldx = ldx;
+  a.w_gate = w_gate;
+  a.w_up = w_up;
+  a.gate = const_cast<void *>(gate);
+  a.up = const_cast<void *>(up);
+  a.lds = lds;
+  a.dh = dh;
+  a.lddh = lddh;
+  a.dx = dx;
+  a.lddx = lddx;
+  a.dw_gate = dw_gate;
+  a.dw_up = dw_up;
+  a.db_gate = db_gate;
+  a.db_up = db_up;
+  return gated_bwd_run(a, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

@@ -1,0 +1,158 @@
+// ezsp_gated.hip -- the gated feed-forward product
+//   g = x Wg + bg,  u = x Wu + bu,  h = act(g) u
+// in one kernel (a block holds the same columns of both products, so the
+// activation and the product happen on its accumulators), and its gradients
+//   dg = dh u act'(g),  du = dh act(g),
+//   dx = dg Wg^T + du Wu^T,  dWg = x^T dg,  dWu = x^T du,  db = row sums.
+// dg and du are formed once, side by side in one table; dx sums over both in
+// one product of twice the length, and both weights' gradients come from one
+// pass over x.
+#include "ezsp_gemm.h"
+
+namespace ezsp {
+
+namespace {
+
+template <class T>
+struct PrepGated {
+  const T *dh, *gate, *up;
+  int64_t lddh, lds;
+  int32_t act;
+  T *dz;  // dg | du, nullable
+  int64_t lddz, half;
+  __device__ __forceinline__ void at(int64_t row, int32_t col, int32_t cnt,
+                                     f32x8_t *v) const {
+    const f32x8_t d = load8(dh + row * lddh + col, cnt);
+    const f32x8_t g = load8(gate + row * lds + col, cnt);
+    const f32x8_t u = load8(up + row * lds + col, cnt);
+    v[0] = d * u * act_grad8(g, act);
+    v[1] = d * act8(g, act);
+  }
+  __device__ __forceinline__ void put(int64_t row, int32_t col, int32_t cnt,
+                                      const f32x8_t *v) const {
+    if (!dz) return;
+    store8(dz + row * lddz + col, v[0], cnt);
+    store8(dz + row * lddz + half + col, v[1], cnt);
+  }
+};
+
+template <class T>
+void forward(const GatedArgs &a, hipStream_t st) {
+  GemmArgs<T> g = {};
+  g.a[0] = g.a[1] = static_cast<const T *>(a.x);
+  g.b[0] = static_cast<const T *>(a.w_gate);
+  g.b[1] = static_cast<const T *>(a.w_up);
+  g.lda = a.ldx;
+  g.ldb = a.d_out;
+  g.m = a.n;
+  g.n = a.d_out;
+  g.k = a.d_in;
+  EpiGated<T> e;
+  e.part = a.part;
+  e.bias[0] = a.b_gate;
+  e.bias[1] = a.b_up;
+  e.h = static_cast<T *>(a.h);
+  e.ldh = a.ldh;
+  e.gate = static_cast<T *>(a.gate);
+  e.up = static_cast<T *>(a.up);
+  e.lds = a.lds;
+  e.act = a.act;
+  gemm<T, true, false, kDual>(g, e, a.part_bytes, st);
+}
+
+template <class T>
+void backward(const GatedArgs &a, hipStream_t st) {
+  const int64_t half = pad_row(a.d_out);
+  T *dz = static_cast<T *>(a.dz);
+  {
+    PrepGated<T> p;
+    p.dh = static_cast<const T *>(a.dh);
+    p.lddh = a.lddh;
+    p.gate = static_cast<const T *>(a.gate);
+    p.up = static_cast<const T *>(a.up);
+    p.lds = a.lds;
+    p.act = a.act;
+    p.dz = a.dx || a.dw_gate || a.dw_up ? dz : nullptr;
+    p.lddz = 2 * half;
+    p.half = half;
+    prep_launch<2>(p, a.n, a.d_out, a.part, a.db_gate, a.db_up, st);
+  }
+  GemmArgs<T> g = {};
+  if (a.dx) {
+    g.a[0] = dz;
+    g.a[1] = dz + half;
+    g.lda = 2 * half;
+    g.b[0] = static_cast<const T *>(a.w_gate);
+    g.b[1] = static_cast<const T *>(a.w_up);
+    g.ldb = a.d_out;
+    g.m = a.n;
+    g.n = a.d_in;
+    g.k = a.d_out;
+    EpiStore<T, 1> e;
+    e.part = a.part;
+    e.out[0] = static_cast<T *>(a.dx);
+    e.ld = a.lddx;
+    gemm<T, true, true, kSeq>(g, e, a.part_bytes, st);
+  }
+  if (a.dw_gate || a.dw_up) {
+    g.a[0] = g.a[1] = static_cast<const T *>(a.x);
+    g.lda = a.ldx;
+    g.b[0] = dz;
+    g.b[1] = dz + half;
+    g.ldb = 2 * half;
+    g.m = a.d_in;
+    g.n = a.d_out;
+    g.k = a.n;
+    EpiStore<T, 2> e;
+    e.part = a.part;
+    e.out[0] = static_cast<T *>(a.dw_gate);
+    e.out[1] = static_cast<T *>(a.dw_up);
+    e.ld = a.d_out;
+    gemm<T, false, false, kDual>(g, e, a.part_bytes, st);
+  }
+}
+
+}  // namespace
+
+void gated_reserve(Arena &ar, int64_t n, int64_t d_in, int64_t d_out,
+                   int32_t type, bool bwd, GatedArgs *a) {
+  a->part_bytes = gemm_part_bytes(d_in, n, d_out, 2);
+  if (bwd) {
+    a->part_bytes =
+        std::max(gemm_part_bytes(2 * d_out, n, d_in, 1),
+                 std::max(gemm_part_bytes(n, d_in, d_out, 2),
+                          (size_t)prep_parts(n) * 2 * (size_t)d_out * 4));
+    a->dz = ar.take<char>((size_t)n * 2 * (size_t)pad_row(d_out) *
+                          type_bytes(type));
+  }
+  a->part = reinterpret_cast<float *>(ar.take<char>(a->part_bytes));
+}
+
+int gated_fwd_run(const GatedArgs &a, hipStream_t st) {
+  prof_begin("gated_ff", st);
+  if (a.type == EZSP_TYPE_BF16)
+    forward<__bf16>(a, st);
+  else
+    forward<float>(a, st);
+  prof_end(st);
+  const double e = (double)type_bytes(a.type);
+  prof_bytes("gated_ff", e * ((double)a.n * (a.d_in + a.d_out *
+                                             (1.0 + (a.gate ? 2.0 : 0.0))) +
+                              2.0 * a.d_in * a.d_out));
+  return check_hip(hipGetLastError(), "gated_ff launch");
+}
+
+int gated_bwd_run(const GatedArgs &a, hipStream_t st) {
+  prof_begin("gated_ff", st);
+  if (a.type == EZSP_TYPE_BF16)
+    backward<__bf16>(a, st);
+  else
+    backward<float>(a, st);
+  prof_end(st);
+  const double e = (double)type_bytes(a.type);
+  prof_bytes("gated_ff", e * ((double)a.n * (2.0 * a.d_in + 3.0 * a.d_out) +
+                              4.0 * a.d_in * a.d_out));
+  return check_hip(hipGetLastError(), "gated_ff backward launch");
+}
+
+}  // namespace ezsp

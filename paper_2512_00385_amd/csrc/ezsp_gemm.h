@@ -1,0 +1,687 @@
+// ezsp_gemm.h -- the matrix products behind the dense operators, on the
+// matrix cores:  D[m][n] = sum over k of A(m, k) B(k, n), fp32 accumulators,
+// with an epilogue applied to each element before its only store.
+//
+// Layouts.  Either operand may be contiguous along k ("K-major": rows of x,
+// rows of dz, and weights [d_in][d_out] seen from dx = dz W^T) or along its
+// own index (weights in y = x W, both operands of dW = x^T dz).  Both come
+// into LDS as they lie in memory, 128 bytes of k at a time (64 bfloat16, 32
+// fp32 values):
+//   K-major  rows of 128 bytes, read as 16-byte pieces along k; piece p of
+//            row r sits at p ^ (r mod 8), so that the 32 rows of a fragment
+//            spread over the banks;
+//   else     one line per k, read through ds_read_b64_tr_b16, which hands
+//            every lane four consecutive k of its own column (fp32: four
+//            separate reads).  A line's 64-byte pieces are exchanged by the
+//            low bits of k for the same reason.
+// The matrix instruction is v_mfma_f32_32x32x16_bf16 (fp32: four
+// v_mfma_f32_32x32x2_f32 over a 16-byte piece each) in transposed form:
+// its rows are n, its columns m, so that a lane's accumulators are runs of
+// four neighbouring columns of D.
+#pragma once
+
+#include <algorithm>
+
+#include "ezsp_dense.h"
+
+namespace ezsp {
+namespace {
+
+// How the two B matrices of an operator enter.
+enum : int {
+  kPlain = 0,  // D = A B0
+  kDual = 1,   // D0 = A B0 and D1 = A B1, both n wide, in one pass over A
+  kSeq = 2,    // D = A0 B0 + A1 B1, the two as one longer sum
+};
+
+template <class T>
+struct GemmArgs {
+  const T *a[2];
+  const T *b[2];
+  int64_t lda, ldb;
+  int32_t m, n, k;  // k of one (A, B) pair
+  int32_t tiles_m, tiles_n;
+  int32_t splits;   // the sum over k in this many parts
+  int32_t kt_split; // LDS tiles of k per part
+};
+
+// Lines that read as zero, for pieces past the end of k.
+static __device__ __attribute__((aligned(16))) const uint32_t kZeroLine[4] = {
+    0, 0, 0, 0};
+
+// Copies 16 bytes a lane from memory into LDS past the registers: lane l's
+// go to lds + 16 l.  Written as instructions because the compiler makes every
+// LDS read after such a copy wait for it, also when it fills another buffer;
+// they write no register, and copies_landed() before the barrier is the wait
+// that the reads need.  The address is base + off, or a full one per lane.
+__device__ __forceinline__ uint32_t lds_addr(const void *lds) {
+  return (uint32_t)(uintptr_t)(
+      (const __attribute__((address_space(3))) void *)lds);
+}
+__device__ __forceinline__ void copy_to_lds16(const void *base, uint32_t off,
+                                              uint32_t lds) {
+  asm volatile(
+      "s_mov_b32 m0, %0\n\ts_nop 0\n\t"
+      "global_load_lds_dwordx4 %1, %2"
+      :
+      : "s"(lds), "v"(off), "s"(base)
+      : "memory", "m0");
+}
+__device__ __forceinline__ void copy_to_lds16(const void *src, uint32_t lds) {
+  asm volatile(
+      "s_mov_b32 m0, %0\n\ts_nop 0\n\t"
+      "global_load_lds_dwordx4 %1, off"
+      :
+      : "s"(lds), "v"(src)
+      : "memory", "m0");
+}
+
+// Waits for this wave's copies into LDS (a barrier alone orders LDS accesses,
+// not these).
+__device__ __forceinline__ void copies_landed() {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+}
+
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef short s16x8_t __attribute__((ext_vector_type(8)));
+
+constexpr int kLineBytes = 128;  // bytes of k in an LDS tile
+
+// One operand's LDS tile: R rows (its own index) by 128 bytes of k.
+template <class T, int R, bool KMAJOR, int NT, bool FAST>
+struct Tile {
+  static constexpr int kPer = 16 / (int)sizeof(T);           // a piece
+  static constexpr int kK = kLineBytes / (int)sizeof(T);      // k of a tile
+  static constexpr int kBytes = R * kLineBytes;
+  static constexpr int kCh = R * 8 / NT;  // pieces a thread moves
+  static constexpr int kLine = R / kPer;  // pieces of a line (not K-major)
+  static_assert(R * 8 % NT == 0, "whole pieces");
+  // exchange of a line's 64-byte pieces
+  static __device__ __forceinline__ int line_swz(int k) {
+    if constexpr (sizeof(T) == 2) {
+      if constexpr (R >= 128) return (k & 3) << 2;
+      if constexpr (R == 64) return ((k >> 1) & 1) << 2;
+    }
+    return 0;
+  }
+
+  uint32_t off[FAST ? kCh : 1];
+  u32x4_t reg[FAST ? 1 : kCh];
+
+  // where piece i of this thread comes from: (row, k) of its first element
+  static __device__ __forceinline__ void place(int i, int &r, int &k) {
+    const int c = i * NT + (int)threadIdx.x;
+    if constexpr (KMAJOR) {
+      r = c >> 3;
+      k = ((c & 7) ^ (r & 7)) * kPer;
+    } else {
+      k = c / kLine;
+      r = ((c % kLine) ^ line_swz(k)) * kPer;
+    }
+  }
+
+  // FAST: byte offsets from the tile's first element.  Rows past the end
+  // repeat the last one: they only feed elements of D that do not exist.
+  __device__ __forceinline__ void init(int32_t rows_left, int64_t ld) {
+    if constexpr (FAST) {
+#pragma unroll
+      for (int i = 0; i < kCh; ++i) {
+        int r, k;
+        place(i, r, k);
+        if constexpr (KMAJOR) {
+          r = min(r, rows_left - 1);
+          off[i] = (uint32_t)(((int64_t)r * ld + k) * (int)sizeof(T));
+        } else {
+          r = min(r, rows_left - kPer);
+          off[i] = (uint32_t)(((int64_t)k * ld + r) * (int)sizeof(T));
+        }
+      }
+    }
+  }
+
+  // Starts bringing in the tile whose first element is p; rows_left and
+  // k_left count what exists from there on.
+  __device__ __forceinline__ void fetch(const T *p, int64_t ld,
+                                        int32_t rows_left, int32_t k_left,
+                                        char *lds) {
+    if constexpr (FAST) {
+      const uint32_t dst = __builtin_amdgcn_readfirstlane(
+          lds_addr(lds) + (threadIdx.x / kWave) * (kWave * 16));
+      if (k_left >= kK) {
+#pragma unroll
+        for (int i = 0; i < kCh; ++i)
+          copy_to_lds16(p, off[i], dst + i * NT * 16);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kCh; ++i) {
+          int r, k;
+          place(i, r, k);
+          const char *src = reinterpret_cast<const char *>(p) + off[i];
+          copy_to_lds16(k < k_left ? src
+                                   : reinterpret_cast<const char *>(kZeroLine),
+                        dst + i * NT * 16);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kCh; ++i) {
+        int r, k;
+        place(i, r, k);
+        const T *q = KMAJOR ? p + (int64_t)r * ld + k : p + (int64_t)k * ld + r;
+        const int32_t along = KMAJOR ? k_left - k : rows_left - r;
+        const bool live = KMAJOR ? r < rows_left : k < k_left;
+        const int32_t cnt = live ? along : 0;
+        u32x4_t v = {0, 0, 0, 0};
+        if (cnt >= kPer) {
+          if constexpr (sizeof(T) == 2)
+            v = *reinterpret_cast<const u32x4_u2 *>(q);
+          else
+            v = *reinterpret_cast<const u32x4_u4 *>(q);
+        } else if (cnt > 0) {
+          if constexpr (sizeof(T) == 2) {
+            const uint16_t *h = reinterpret_cast<const uint16_t *>(q);
+#pragma unroll
+            for (int e = 0; e < kPer; ++e)
+              if (e < cnt) v[e / 2] |= (uint32_t)h[e] << (16 * (e & 1));
+          } else {
+            const uint32_t *h = reinterpret_cast<const uint32_t *>(q);
+#pragma unroll
+            for (int e = 0; e < kPer; ++e)
+              if (e < cnt) v[e] = h[e];
+          }
+        }
+        reg[i] = v;
+      }
+    }
+  }
+
+  // Ends it where the pieces went through registers.
+  __device__ __forceinline__ void put(char *lds) {
+    if constexpr (!FAST) {
+#pragma unroll
+      for (int i = 0; i < kCh; ++i)
+        *reinterpret_cast<u32x4_t *>(lds +
+                                     (i * NT + (int)threadIdx.x) * 16) =
+            reg[i];
+    }
+  }
+
+  // Fragment of rows row0 .. row0 + 31 (row0 a multiple of 32) and k step s:
+  // lane l gets piece 2 s + l / 32 of row row0 + l % 32.
+  static __device__ __forceinline__ u32x4_t frag(const char *lds, int row0,
+                                                 int s, int lane) {
+    if constexpr (KMAJOR) {
+      const int piece = (2 * s + (lane >> 5)) ^ (lane & 7);
+      return *reinterpret_cast<const u32x4_t *>(
+          lds + (row0 + (lane & 31)) * kLineBytes + piece * 16);
+    } else if constexpr (sizeof(T) == 2) {
+      const int q = (lane & 15) >> 2;
+      const int k = 16 * s + 8 * (lane >> 5) + q;
+      const int byte = (((row0 >> 3) ^ line_swz(q)) << 4) +
+                       32 * ((lane >> 4) & 1) + 8 * (lane & 3);
+      const char *at = lds + k * (R * 2) + byte;
+      typedef __attribute__((address_space(3))) s16x4_t *lds_ptr;
+      const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)at);
+      const s16x4_t hi =
+          __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_ptr)(at + 4 * R * 2));
+      const s16x8_t both =
+          __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      return __builtin_bit_cast(u32x4_t, both);
+    } else {
+      const float *f = reinterpret_cast<const float *>(lds) + row0 +
+                       (lane & 31) + (8 * s + 4 * (lane >> 5)) * R;
+      u32x4_t v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = __float_as_uint(f[e * R]);
+      return v;
+    }
+  }
+};
+
+template <class T>
+__device__ __forceinline__ f32x16_t mma(u32x4_t n_frag, u32x4_t m_frag,
+                                        f32x16_t acc) {
+  if constexpr (sizeof(T) == 2) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+        __builtin_bit_cast(bf16x8_t, n_frag),
+        __builtin_bit_cast(bf16x8_t, m_frag), acc, 0, 0, 0);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      acc = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(n_frag[e]),
+                                                 __uint_as_float(m_frag[e]),
+                                                 acc, 0, 0, 0);
+    return acc;
+  }
+}
+
+// Block of WM x WN waves on a tile of BM x BN of D (kDual: BN / 2 columns of
+// each product side by side).
+template <class T_, int BM_, int BN_, int WM_, int WN_, bool AK_, bool BK_,
+          int MODE_, bool FAST_>
+struct Shape {
+  typedef T_ T;
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, MODE = MODE_;
+  static constexpr bool AK = AK_, BK = BK_, FAST = FAST_;
+  static constexpr int NT = WM * WN * kWave;
+  static constexpr int TM = BM / WM / 32, TN = BN / WN / 32;  // of a wave
+  static constexpr int NB = MODE == kDual ? 2 : 1;
+  static constexpr int CN = BN / NB;   // columns of D of a tile
+  static constexpr int WC = TN * 32 / NB;  // ... and of a wave
+  typedef Tile<T, BM, AK, NT, FAST> TileA;
+  typedef Tile<T, CN, BK, NT, FAST> TileB;
+  static constexpr int kK = TileA::kK;
+  static constexpr int kStage = (BM + BN) * kLineBytes;
+  static_assert(MODE != kDual || TN % 2 == 0, "both products in a wave");
+  // epilogue: 32 rows of a wave's columns
+  static constexpr int kOutLd = TN * 32 + 4;
+  static constexpr int kOut = 32 * kOutLd * 4;
+  static_assert(WM * WN * kOut <= 2 * kStage, "epilogue fits the stages");
+};
+
+// Logical tile of block b out of total: XCD x takes the x-th contiguous run
+// (blocks are dealt to the XCDs in turn), and inside it tiles go in bands of
+// kBand tile rows, so that a band's A rows and the B columns it meets stay in
+// that XCD's L2.
+constexpr int kBand = 8;
+__device__ __forceinline__ void tile_of(int32_t b, int32_t total,
+                                        int32_t tiles_m, int32_t tiles_n,
+                                        int32_t &tm, int32_t &tn, int32_t &sp) {
+  const int32_t per = total / kXcd, extra = total % kXcd;
+  const int32_t x = b % kXcd, j = b / kXcd;
+  int32_t t = x * per + min(x, extra) + j;
+  const int32_t tiles = tiles_m * tiles_n;
+  sp = t / tiles;
+  t -= sp * tiles;
+  const int32_t band = t / (kBand * tiles_n);
+  const int32_t rows = min(kBand, tiles_m - band * kBand);
+  const int32_t in = t - band * kBand * tiles_n;
+  tm = band * kBand + in % rows;
+  tn = in / rows;
+}
+
+template <class S, class Epi>
+__global__ __launch_bounds__(S::NT) void k_gemm(GemmArgs<typename S::T> g,
+                                                Epi epi) {
+  typedef typename S::T T;
+  __shared__ __attribute__((aligned(16))) char stages[2 * S::kStage];
+  const int lane = threadIdx.x & (kWave - 1);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int wm = wave / S::WN, wn = wave % S::WN;
+  const int32_t total = g.tiles_m * g.tiles_n * g.splits;
+  const int32_t kt1 = (g.k + S::kK - 1) / S::kK;  // LDS tiles of one pair
+  const int32_t kt_all = S::MODE == kSeq ? 2 * kt1 : kt1;
+
+  for (int32_t blk = blockIdx.x; blk < total; blk += gridDim.x) {
+    int32_t tm, tn, sp;
+    tile_of(blk, total, g.tiles_m, g.tiles_n, tm, tn, sp);
+    const int32_t m0 = tm * S::BM, n0 = tn * S::CN;
+    const int32_t t_begin = sp * g.kt_split;
+    const int32_t t_end = min(kt_all, t_begin + g.kt_split);
+    typename S::TileA ta;
+    typename S::TileB tb[S::NB];
+    ta.init(g.m - m0, g.lda);
+#pragma unroll
+    for (int p = 0; p < S::NB; ++p) tb[p].init(g.n - n0, g.ldb);
+
+    auto fetch = [&](int32_t t, char *st) {
+      const bool second = S::MODE == kSeq && t >= kt1;
+      const int32_t k0 = (second ? t - kt1 : t) * S::kK;
+      const T *a = second ? g.a[1] : g.a[0];
+      ta.fetch(S::AK ? a + (int64_t)m0 * g.lda + k0
+                     : a + (int64_t)k0 * g.lda + m0,
+               g.lda, g.m - m0, g.k - k0, st);
+#pragma unroll
+      for (int p = 0; p < S::NB; ++p) {
+        const T *b = (second || p) ? g.b[1] : g.b[0];
+        tb[p].fetch(S::BK ? b + (int64_t)n0 * g.ldb + k0
+                          : b + (int64_t)k0 * g.ldb + n0,
+                    g.ldb, g.n - n0, g.k - k0,
+                    st + S::TileA::kBytes + p * S::TileB::kBytes);
+      }
+    };
+    auto put = [&](char *st) {
+      ta.put(st);
+#pragma unroll
+      for (int p = 0; p < S::NB; ++p)
+        tb[p].put(st + S::TileA::kBytes + p * S::TileB::kBytes);
+    };
+
+    f32x16_t acc[S::TM][S::TN];
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+      for (int j = 0; j < S::TN; ++j) acc[i][j] = f32x16_t(0.0f);
+
+    auto compute = [&](const char *st) {
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        u32x4_t fa[S::TM], fb[S::TN];
+#pragma unroll
+        for (int i = 0; i < S::TM; ++i)
+          fa[i] = S::TileA::frag(st, (wm * S::TM + i) * 32, s, lane);
+#pragma unroll
+        for (int j = 0; j < S::TN; ++j) {
+          const int p = j / (S::TN / S::NB), jj = j % (S::TN / S::NB);
+          fb[j] = S::TileB::frag(
+              st + S::TileA::kBytes + p * S::TileB::kBytes,
+              wn * S::WC + jj * 32, s, lane);
+        }
+#pragma unroll
+        for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+          for (int j = 0; j < S::TN; ++j)
+            acc[i][j] = mma<T>(fb[j], fa[i], acc[i][j]);
+      }
+    };
+
+    int32_t cur = 0;
+    fetch(t_begin, stages);
+    put(stages);
+    copies_landed();
+    __syncthreads();
+    for (int32_t t = t_begin; t < t_end; ++t) {
+      char *next = stages + (S::kStage - cur);
+      if (t + 1 < t_end) fetch(t + 1, next);
+      compute(stages + cur);
+      if (t + 1 < t_end) put(next);
+      copies_landed();
+      __syncthreads();
+      cur = S::kStage - cur;
+    }
+
+    // epilogue: 32 rows at a time through the wave's own part of LDS, so
+    // that each lane ends up with kVec neighbouring columns of a row
+    float *out = reinterpret_cast<float *>(stages + wave * S::kOut);
+    constexpr int kLanes = S::WC / kVec;  // lanes of a row
+    const int32_t col = n0 + wn * S::WC + (lane % kLanes) * kVec;
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i) {
+#pragma unroll
+      for (int j = 0; j < S::TN; ++j)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          f32x4_t v;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = acc[i][j][4 * q + e];
+          *reinterpret_cast<f32x4_t *>(out + (lane & 31) * S::kOutLd + j * 32 +
+                                       8 * q + 4 * (lane >> 5)) = v;
+        }
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int pass = 0; pass < 32 * kLanes / kWave; ++pass) {
+        const int r = pass * (kWave / kLanes) + lane / kLanes;
+        const int32_t row = m0 + (wm * S::TM + i) * 32 + r;
+        const float *src = out + r * S::kOutLd + (lane % kLanes) * kVec;
+        f32x8_t v[S::NB];
+#pragma unroll
+        for (int p = 0; p < S::NB; ++p) {
+          const f32x4_t lo =
+              *reinterpret_cast<const f32x4_t *>(src + p * S::WC);
+          const f32x4_t hi =
+              *reinterpret_cast<const f32x4_t *>(src + p * S::WC + 4);
+          v[p] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+        if (row < g.m && col < g.n) {
+          if (g.splits == 1)
+            epi.apply(row, col, g.n - col, v);
+          else
+            epi.partial(sp, g.m, g.n, row, col, v);
+        }
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+    __syncthreads();  // the stages are free again
+  }
+}
+
+// The parts of a split sum, added in order, through the epilogue.
+template <int NB, class Epi>
+__global__ __launch_bounds__(256) void k_gemm_join(int32_t splits, int32_t m,
+                                                   int32_t n, Epi epi) {
+  const int32_t per_row = (n + kVec - 1) / kVec;
+  const int64_t items = (int64_t)m * per_row;
+  for (int64_t it = (int64_t)blockIdx.x * 256 + threadIdx.x; it < items;
+       it += (int64_t)gridDim.x * 256) {
+    const int32_t row = (int32_t)(it / per_row);
+    const int32_t col = (int32_t)(it % per_row) * kVec;
+    f32x8_t v[NB];
+#pragma unroll
+    for (int p = 0; p < NB; ++p) v[p] = f32x8_t(0.0f);
+    for (int32_t s = 0; s < splits; ++s)
+#pragma unroll
+      for (int p = 0; p < NB; ++p)
+        v[p] += load8(epi.part +
+                          (((int64_t)s * NB + p) * m + row) * n + col,
+                      n - col);
+    epi.apply(row, col, n - col, v);
+  }
+}
+
+// --- epilogues --------------------------------------------------------------
+template <int NB>
+struct EpiParts {
+  float *part;  // [split][product][m][n]
+  __device__ __forceinline__ void partial(int32_t sp, int32_t m, int32_t n,
+                                          int32_t row, int32_t col,
+                                          const f32x8_t *v) const {
+#pragma unroll
+    for (int p = 0; p < NB; ++p)
+      store8(part + (((int64_t)sp * NB + p) * m + row) * n + col, v[p],
+             n - col);
+  }
+};
+
+// y = act(acc + bias) + residual, z = acc + bias
+struct EpiLinear : EpiParts<1> {
+  const float *bias;
+  const void *res;
+  int64_t ldr;
+  void *y;
+  int64_t ldy;
+  void *z;
+  int64_t ldz;
+  int32_t type, type_y, act;
+  __device__ __forceinline__ void apply(int32_t row, int32_t col, int32_t cnt,
+                                        f32x8_t *v) const {
+    if (bias) v[0] += load8(bias + col, cnt);
+    if (z) store8_t(z, row * ldz + col, type, v[0], cnt);
+    f32x8_t o = act8(v[0], act);
+    if (res) o += load8_t(res, row * ldr + col, type_y, cnt);
+    store8_t(y, row * ldy + col, type_y, o, cnt);
+  }
+};
+
+// h = act(acc0 + bias0) * (acc1 + bias1), and the two sums
+template <class T>
+struct EpiGated : EpiParts<2> {
+  const float *bias[2];
+  T *h, *gate, *up;
+  int64_t ldh, lds;
+  int32_t act;
+  __device__ __forceinline__ void apply(int32_t row, int32_t col, int32_t cnt,
+                                        f32x8_t *v) const {
+#pragma unroll
+    for (int p = 0; p < 2; ++p)
+      if (bias[p]) v[p] += load8(bias[p] + col, cnt);
+    if (gate) store8(gate + row * lds + col, v[0], cnt);
+    if (up) store8(up + row * lds + col, v[1], cnt);
+    store8(h + row * ldh + col, act8(v[0], act) * v[1], cnt);
+  }
+};
+
+// one or two plain results
+template <class T, int NB>
+struct EpiStore : EpiParts<NB> {
+  T *out[NB];
+  int64_t ld;
+  __device__ __forceinline__ void apply(int32_t row, int32_t col, int32_t cnt,
+                                        f32x8_t *v) const {
+#pragma unroll
+    for (int p = 0; p < NB; ++p)
+      if (out[p]) store8(out[p] + row * ld + col, v[p], cnt);
+  }
+};
+
+// --- launch -----------------------------------------------------------------
+inline bool fast_operand(const void *p, int64_t ld, int32_t contiguous,
+                         int32_t bytes) {
+  return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld * bytes % 16 == 0 &&
+         contiguous * bytes % 16 == 0 && ld < ((int64_t)1 << 21);
+}
+
+template <class S, class Epi>
+void gemm_launch(GemmArgs<typename S::T> g, const Epi &epi, int32_t splits,
+                 hipStream_t st) {
+  g.tiles_m = (g.m + S::BM - 1) / S::BM;
+  g.tiles_n = (g.n + S::CN - 1) / S::CN;
+  const int32_t kt = (g.k + S::kK - 1) / S::kK * (S::MODE == kSeq ? 2 : 1);
+  g.splits = splits;
+  g.kt_split = (kt + splits - 1) / splits;
+  g.splits = (kt + g.kt_split - 1) / g.kt_split;  // no empty part
+  const int64_t total = (int64_t)g.tiles_m * g.tiles_n * g.splits;
+  hipLaunchKernelGGL((k_gemm<S, Epi>),
+                     dim3((unsigned)std::min<int64_t>(total, 1 << 21)),
+                     dim3(S::NT), 0, st, g, epi);
+  if (g.splits > 1) {
+    const int64_t items = (int64_t)g.m * ((g.n + kVec - 1) / kVec);
+    hipLaunchKernelGGL((k_gemm_join<S::NB, Epi>),
+                       dim3((unsigned)std::min<int64_t>((items + 255) / 256,
+                                                        1 << 16)),
+                       dim3(256), 0, st, g.splits, g.m, g.n, epi);
+  }
+}
+
+// Splits of a sum over k for a product of `tiles` tiles: enough blocks for
+// two a CU, four LDS tiles a part at least, and no more parts than the
+// workspace holds.
+template <class S>
+int32_t gemm_splits(const GemmArgs<typename S::T> &g, size_t part_bytes) {
+  const int64_t tiles = (int64_t)((g.m + S::BM - 1) / S::BM) *
+                        ((g.n + S::CN - 1) / S::CN);
+  const int64_t kt = ((int64_t)g.k + S::kK - 1) / S::kK *
+                     (S::MODE == kSeq ? 2 : 1);
+  const int64_t one = (int64_t)g.m * g.n * S::NB * 4;
+  int64_t s = std::min<int64_t>(512 / std::max<int64_t>(tiles, 1), kt / 4);
+  s = std::min<int64_t>(s, (int64_t)(part_bytes / (size_t)one));
+  return (int32_t)std::max<int64_t>(s, 1);
+}
+
+// Tile of the block by the shape of D.
+template <class T, bool AK, bool BK, int MODE, bool FAST, class Epi>
+void gemm_shape(const GemmArgs<T> &g, const Epi &epi, size_t part_bytes,
+                hipStream_t st) {
+#define EZSP_GEMM(BM, BN, WM, WN)                                          \
+  do {                                                                     \
+    typedef Shape<T, BM, BN, WM, WN, AK, BK, MODE, FAST> S;                \
+    gemm_launch<S>(g, epi, gemm_splits<S>(g, part_bytes), st);             \
+    return;                                                                \
+  } while (0)
+  constexpr int kB = MODE == kDual ? 2 : 1;
+  if (g.m <= 32) EZSP_GEMM(32, 128, 1, kB == 2 ? 2 : 4);
+  if (g.n <= 32) EZSP_GEMM(128, 32 * kB, 4, 1);
+  if (g.n * kB <= 64) EZSP_GEMM(128, 64, 4, 1);
+  if constexpr (FAST && sizeof(T) == 2) {
+    const int64_t big = (int64_t)((g.m + 255) / 256) *
+                        ((g.n * kB + 255) / 256);
+    if (big >= 192) EZSP_GEMM(256, 256, 2, 4);
+  }
+  EZSP_GEMM(128, 128, 2, 2);
+#undef EZSP_GEMM
+}
+
+// D = A B through epi; part_bytes is what epi.part holds.
+template <class T, bool AK, bool BK, int MODE, class Epi>
+void gemm(const GemmArgs<T> &g, const Epi &epi, size_t part_bytes,
+          hipStream_t st) {
+  const int32_t e = (int32_t)sizeof(T);
+  bool fast = fast_operand(g.a[0], g.lda, AK ? g.k : g.m, e) &&
+              fast_operand(g.b[0], g.ldb, BK ? g.k : g.n, e);
+  if (MODE == kSeq) fast = fast && fast_operand(g.a[1], g.lda, AK ? g.k : g.m, e);
+  if (MODE != kPlain)
+    fast = fast && fast_operand(g.b[1], g.ldb, BK ? g.k : g.n, e);
+  if (fast)
+    gemm_shape<T, AK, BK, MODE, true>(g, epi, part_bytes, st);
+  else
+    gemm_shape<T, AK, BK, MODE, false>(g, epi, part_bytes, st);
+}
+
+// --- gradients before their products ---------------------------------------
+// Op::at gives the gradients of NB pre-activations at kVec neighbouring
+// columns of a row, Op::put stores them; the column sums (the biases'
+// gradients) are kept in registers over a block's rows, in fp32 and before
+// any rounding, and joined over the block: part[block row][NB * m].
+constexpr int kPrepNT = 256;
+constexpr int kPrepCols = 16;                    // column groups of a block
+constexpr int kPrepRows = kPrepNT / kPrepCols;   // rows of a step
+constexpr int32_t kPrepParts = 512;
+
+template <int NB, class Op>
+__global__ __launch_bounds__(kPrepNT) void k_prep(Op op, int32_t n, int32_t m,
+                                                  float *__restrict__ part) {
+  __shared__ float red[kPrepNT / kWave][kPrepCols][kVec];
+  const int cg = threadIdx.x % kPrepCols, rg = threadIdx.x / kPrepCols;
+  const int32_t col = ((int32_t)blockIdx.x * kPrepCols + cg) * kVec;
+  f32x8_t sum[NB];
+#pragma unroll
+  for (int p = 0; p < NB; ++p) sum[p] = f32x8_t(0.0f);
+  if (col < m) {
+    for (int64_t row = (int64_t)blockIdx.y * kPrepRows + rg; row < n;
+         row += (int64_t)gridDim.y * kPrepRows) {
+      f32x8_t v[NB];
+      op.at(row, col, m - col, v);
+      op.put(row, col, m - col, v);
+#pragma unroll
+      for (int p = 0; p < NB; ++p) sum[p] += v[p];
+    }
+  }
+  if (!part) return;
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+#pragma unroll
+  for (int p = 0; p < NB; ++p) {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) {
+      sum[p][i] += __shfl_xor(sum[p][i], 16, kWave);
+      sum[p][i] += __shfl_xor(sum[p][i], 32, kWave);
+      if (lane < kPrepCols) red[wave][cg][i] = sum[p][i];
+    }
+    __syncthreads();
+    if (threadIdx.x < kPrepCols * kVec) {
+      const int c = threadIdx.x / kVec, i = threadIdx.x % kVec;
+      const int32_t at = ((int32_t)blockIdx.x * kPrepCols + c) * kVec + i;
+      float t = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kPrepNT / kWave; ++w) t += red[w][c][i];
+      if (at < m) part[((int64_t)blockIdx.y * NB + p) * m + at] = t;
+    }
+    __syncthreads();
+  }
+}
+
+inline int32_t prep_parts(int64_t n) {
+  return (int32_t)std::min<int64_t>((n + kPrepRows - 1) / kPrepRows,
+                                    kPrepParts);
+}
+
+template <int NB, class Op>
+void prep_launch(const Op &op, int32_t n, int32_t m, float *part,
+                 float *db0, float *db1, hipStream_t st) {
+  const bool sums = db0 || db1;
+  const int32_t parts = prep_parts(n);
+  const int32_t bx = (m + kPrepCols * kVec - 1) / (kPrepCols * kVec);
+  hipLaunchKernelGGL((k_prep<NB, Op>), dim3((unsigned)bx, (unsigned)parts),
+                     dim3(kPrepNT), 0, st, op, n, m, sums ? part : nullptr);
+  if (sums) join_rows(part, parts, NB * m, db0, db1, m, st);
+}
+
+// Bytes for the parts of a split product of m x n results: every part of a
+// small product, at most 128 MiB (the splits then follow).  Grows with each
+// argument.
+inline size_t gemm_part_bytes(int64_t k, int64_t m, int64_t n, int products) {
+  const int64_t parts = std::min<int64_t>(512, (k + 127) / 128 * products);
+  const double want = 4.0 * (double)parts * (double)m * (double)n * products;
+  return (size_t)std::min<double>(want, (double)((size_t)128 << 20)) + 256;
+}
+
+}  // namespace
+}  // namespace ezsp

@@ -257,6 +257,62 @@ constexpr int32_t kNormParts = 1024;
 int norm_fwd_run(const NormArgs &a, hipStream_t st);
 int norm_bwd_run(const NormArgs &a, hipStream_t st);
 
+// Length of a row of a workspace matrix: whole 16-byte pieces of any type.
+inline int64_t pad_row(int64_t d) { return (d + 7) & ~(int64_t)7; }
+
+// y = act(x W + b) + residual, forward and backward.
+struct LinearArgs {
+  int32_t n, d_in, d_out;
+  int32_t type, type_y, act;
+  const void *x, *w;
+  int64_t ldx;
+  const float *bias;   // nullable
+  const void *res;     // nullable
+  int64_t ldr;
+  void *y;             // forward
+  int64_t ldy;
+  void *z;             // forward: out, nullable; backward: in
+  int64_t ldz;
+  const void *dy;      // backward
+  int64_t lddy;
+  void *dx, *dw;       // nullable
+  int64_t lddx;
+  float *db;           // nullable
+  void *dz;            // workspace: n rows of pad_row(d_out)
+  float *part;         // workspace: parts of split sums
+  size_t part_bytes;
+};
+void linear_reserve(Arena &ar, int64_t n, int64_t d_in, int64_t d_out,
+                    int32_t type, bool bwd, LinearArgs *a);
+int linear_fwd_run(const LinearArgs &a, hipStream_t st);
+int linear_bwd_run(const LinearArgs &a, hipStream_t st);
+
+// h = act(x Wg + bg) * (x Wu + bu), forward and backward.
+struct GatedArgs {
+  int32_t n, d_in, d_out;
+  int32_t type, act;
+  const void *x, *w_gate, *w_up;
+  int64_t ldx;
+  const float *b_gate, *b_up;   // nullable
+  void *h;                      // forward
+  int64_t ldh;
+  void *gate, *up;              // forward: out, nullable; backward: in
+  int64_t lds;
+  const void *dh;               // backward
+  int64_t lddh;
+  void *dx;                     // nullable
+  int64_t lddx;
+  void *dw_gate, *dw_up;        // nullable
+  float *db_gate, *db_up;       // nullable
+  void *dz;                     // workspace: n rows of 2 * pad_row(d_out)
+  float *part;
+  size_t part_bytes;
+};
+void gated_reserve(Arena &ar, int64_t n, int64_t d_in, int64_t d_out,
+                   int32_t type, bool bwd, GatedArgs *a);
+int gated_fwd_run(const GatedArgs &a, hipStream_t st);
+int gated_bwd_run(const GatedArgs &a, hipStream_t st);
+
 // Shared host helpers.
 void set_error(const char *fmt, ...);
 int read_ctl(Ctl *ctl, Ctl *host, hipStream_t st);  // sync + copy back

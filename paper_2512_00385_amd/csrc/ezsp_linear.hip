@@ -1,0 +1,160 @@
+// ezsp_linear.hip -- y = act(x W + b) + residual and its gradients
+//   dz = dy act'(z),  dx = dz W^T,  dW = x^T dz,  db = sum over rows of dz.
+// The forward pass is one matrix product with everything else in its
+// epilogue.  Backward, dz is formed once (both products read it) with the
+// bias's sums on the way; for bfloat16 it is rounded there, since the matrix
+// cores take it so, while db is summed from the unrounded values.
+#include "ezsp_gemm.h"
+
+namespace ezsp {
+
+namespace {
+
+template <class T>
+struct PrepLinear {
+  const void *dy;
+  int64_t lddy;
+  int32_t type_y;
+  const T *z;  // nullable with EZSP_ACT_NONE
+  int64_t ldz;
+  int32_t act;
+  T *dz;       // nullable: dy itself serves
+  int64_t lddz;
+  __device__ __forceinline__ void at(int64_t row, int32_t col, int32_t cnt,
+                                     f32x8_t *v) const {
+    v[0] = load8_t(dy, row * lddy + col, type_y, cnt);
+    if (act != EZSP_ACT_NONE)
+      v[0] *= act_grad8(load8(z + row * ldz + col, cnt), act);
+  }
+  __device__ __forceinline__ void put(int64_t row, int32_t col, int32_t cnt,
+                                      const f32x8_t *v) const {
+    if (dz) store8(dz + row * lddz + col, v[0], cnt);
+  }
+};
+
+// dz has to be formed unless dy is it already
+bool needs_dz(const LinearArgs &a) {
+  return a.act != EZSP_ACT_NONE || a.type_y != a.type;
+}
+
+template <class T>
+void forward(const LinearArgs &a, hipStream_t st) {
+  GemmArgs<T> g = {};
+  g.a[0] = static_cast<const T *>(a.x);
+  g.b[0] = static_cast<const T *>(a.w);
+  g.lda = a.ldx;
+  g.ldb = a.d_out;
+  g.m = a.n;
+  g.n = a.d_out;
+  g.k = a.d_in;
+  EpiLinear e;
+  e.part = a.part;
+  e.bias = a.bias;
+  e.res = a.res;
+  e.ldr = a.ldr;
+  e.y = a.y;
+  e.ldy = a.ldy;
+  e.z = a.z;
+  e.ldz = a.ldz;
+  e.type = a.type;
+  e.type_y = a.type_y;
+  e.act = a.act;
+  gemm<T, true, false, kPlain>(g, e, a.part_bytes, st);
+}
+
+template <class T>
+void backward(const LinearArgs &a, hipStream_t st) {
+  const bool form = needs_dz(a) && (a.dx || a.dw);
+  const T *dz = static_cast<const T *>(a.dy);
+  int64_t lddz = a.lddy;
+  if (form || a.db) {
+    PrepLinear<T> p;
+    p.dy = a.dy;
+    p.lddy = a.lddy;
+    p.type_y = a.type_y;
+    p.z = static_cast<const T *>(a.z);
+    p.ldz = a.ldz;
+    p.act = a.act;
+    p.dz = form ? static_cast<T *>(a.dz) : nullptr;
+    p.lddz = pad_row(a.d_out);
+    prep_launch<1>(p, a.n, a.d_out, a.part, a.db, nullptr, st);
+  }
+  if (form) {
+    dz = static_cast<const T *>(a.dz);
+    lddz = pad_row(a.d_out);
+  }
+  EpiStore<T, 1> e;
+  e.part = a.part;
+  GemmArgs<T> g = {};
+  if (a.dx) {
+    g.a[0] = dz;
+    g.lda = lddz;
+    g.b[0] = static_cast<const T *>(a.w);
+    g.ldb = a.d_out;
+    g.m = a.n;
+    g.n = a.d_in;
+    g.k = a.d_out;
+    e.out[0] = static_cast<T *>(a.dx);
+    e.ld = a.lddx;
+    gemm<T, true, true, kPlain>(g, e, a.part_bytes, st);
+  }
+  if (a.dw) {
+    g.a[0] = static_cast<const T *>(a.x);
+    g.lda = a.ldx;
+    g.b[0] = dz;
+    g.ldb = lddz;
+    g.m = a.d_in;
+    g.n = a.d_out;
+    g.k = a.n;
+    e.out[0] = static_cast<T *>(a.dw);
+    e.ld = a.d_out;
+    gemm<T, false, false, kPlain>(g, e, a.part_bytes, st);
+  }
+}
+
+}  // namespace
+
+void linear_reserve(Arena &ar, int64_t n, int64_t d_in, int64_t d_out,
+                    int32_t type, bool bwd, LinearArgs *a) {
+  a->part_bytes = gemm_part_bytes(d_in, n, d_out, 1);
+  if (bwd) {
+    a->part_bytes =
+        std::max(gemm_part_bytes(d_out, n, d_in, 1),
+                 std::max(gemm_part_bytes(n, d_in, d_out, 1),
+                          (size_t)prep_parts(n) * (size_t)d_out * 4));
+    a->dz = ar.take<char>((size_t)n * (size_t)pad_row(d_out) *
+                          type_bytes(type));
+  }
+  a->part = reinterpret_cast<float *>(ar.take<char>(a->part_bytes));
+}
+
+int linear_fwd_run(const LinearArgs &a, hipStream_t st) {
+  prof_begin("linear", st);
+  if (a.type == EZSP_TYPE_BF16)
+    forward<__bf16>(a, st);
+  else
+    forward<float>(a, st);
+  prof_end(st);
+  const double e = (double)type_bytes(a.type), y = (double)type_bytes(a.type_y);
+  prof_bytes("linear", (double)a.n * (a.d_in * e + a.d_out *
+                                      (y + (a.res ? y : 0.0) +
+                                       (a.z ? e : 0.0))) +
+                           (double)a.d_in * a.d_out * e);
+  return check_hip(hipGetLastError(), "linear launch");
+}
+
+int linear_bwd_run(const LinearArgs &a, hipStream_t st) {
+  prof_begin("linear", st);
+  if (a.type == EZSP_TYPE_BF16)
+    backward<__bf16>(a, st);
+  else
+    backward<float>(a, st);
+  prof_end(st);
+  const double e = (double)type_bytes(a.type), y = (double)type_bytes(a.type_y);
+  prof_bytes("linear", (double)a.n * (a.d_in * 2 * e + a.d_out *
+                                      (y + (a.z ? e : 0.0))) +
+                           2.0 * a.d_in * a.d_out * e);
+  return check_hip(hipGetLastError(), "linear backward launch");
+}
+
+}  // namespace ezsp

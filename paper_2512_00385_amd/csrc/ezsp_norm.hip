@@ -21,6 +21,7 @@ namespace ezsp {
 namespace {
 
 constexpr int kNormNT = 256;
+constexpr int64_t kNormGrid = (int64_t)1 << 22;  // blocks of a launch
 
 // Sum over the G lanes of a group, in each of them (G = kNormNT: a block;
 // red is LDS of 2 * kNormNT / kWave floats, used in turn).
@@ -49,49 +50,51 @@ __global__ __launch_bounds__(kNormNT) void k_norm_fwd(
     float *__restrict__ rstd_out) {
   __shared__ float red[kNormNT / kWave];
   const int gl = threadIdx.x % G;
-  const int64_t row =
-      (int64_t)blockIdx.x * (kNormNT / G) + threadIdx.x / G;
-  const bool live = row < n;
-  const TX *xr = x + (live ? row : 0) * ldx;
-  f32x8_t v[NV];
-  float s = 0.0f;
+  for (int64_t r0 = (int64_t)blockIdx.x * (kNormNT / G); r0 < n;
+       r0 += (int64_t)gridDim.x * (kNormNT / G)) {
+    const int64_t row = r0 + threadIdx.x / G;
+    const bool live = row < n;
+    const TX *xr = x + (live ? row : 0) * ldx;
+    f32x8_t v[NV];
+    float s = 0.0f;
 #pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    const int c = (gl + G * j) * kVec;
-    v[j] = load8(xr + c, live ? d - c : 0);
+    for (int j = 0; j < NV; ++j) {
+      const int c = (gl + G * j) * kVec;
+      v[j] = load8(xr + c, live ? d - c : 0);
 #pragma unroll
-    for (int i = 0; i < kVec; ++i) s += v[j][i];
-  }
-  const float inv_d = 1.0f / (float)d;
-  const float mean = group_sum<G>(s, red) * inv_d;
-  float q = 0.0f;
-#pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    const int c = (gl + G * j) * kVec;
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) {
-      const float t = v[j][i] - mean;
-      q += c + i < d ? t * t : 0.0f;
+      for (int i = 0; i < kVec; ++i) s += v[j][i];
     }
-  }
-  const float rstd = 1.0f / sqrtf(group_sum<G>(q, red) * inv_d + eps);
-  if (!live) return;
-  TY *yr = y + row * ldy;
+    const float inv_d = 1.0f / (float)d;
+    const float mean = group_sum<G>(s, red) * inv_d;
+    float q = 0.0f;
 #pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    const int c = (gl + G * j) * kVec;
-    if (c >= d) break;
-    f32x8_t o;
-    const f32x8_t wv = w ? load8(w + c, d - c) : f32x8_t(1.0f);
-    const f32x8_t bv = b ? load8(b + c, d - c) : f32x8_t(0.0f);
+    for (int j = 0; j < NV; ++j) {
+      const int c = (gl + G * j) * kVec;
 #pragma unroll
-    for (int i = 0; i < kVec; ++i)
-      o[i] = (v[j][i] - mean) * rstd * wv[i] + bv[i];
-    store8(yr + c, o, d - c);
-  }
-  if (gl == 0) {
-    if (mean_out) mean_out[row] = mean;
-    if (rstd_out) rstd_out[row] = rstd;
+      for (int i = 0; i < kVec; ++i) {
+        const float t = v[j][i] - mean;
+        q += c + i < d ? t * t : 0.0f;
+      }
+    }
+    const float rstd = 1.0f / sqrtf(group_sum<G>(q, red) * inv_d + eps);
+    if (!live) continue;
+    TY *yr = y + row * ldy;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int c = (gl + G * j) * kVec;
+      if (c >= d) break;
+      f32x8_t o;
+      const f32x8_t wv = w ? load8(w + c, d - c) : f32x8_t(1.0f);
+      const f32x8_t bv = b ? load8(b + c, d - c) : f32x8_t(0.0f);
+#pragma unroll
+      for (int i = 0; i < kVec; ++i)
+        o[i] = (v[j][i] - mean) * rstd * wv[i] + bv[i];
+      store8(yr + c, o, d - c);
+    }
+    if (gl == 0) {
+      if (mean_out) mean_out[row] = mean;
+      if (rstd_out) rstd_out[row] = rstd;
+    }
   }
 }
 
@@ -251,8 +254,9 @@ template <class TX, class TY, int G, int NV>
 void fwd(const NormArgs &a, hipStream_t st) {
   const int64_t rows = kNormNT / G;
   hipLaunchKernelGGL((k_norm_fwd<TX, TY, G, NV>),
-                     dim3((unsigned)((a.n + rows - 1) / rows)), dim3(kNormNT),
-                     0, st, static_cast<const TX *>(a.x), a.ldx, a.n, a.d, a.w,
+                     dim3((unsigned)std::min<int64_t>(
+                         (a.n + rows - 1) / rows, kNormGrid)),
+                     dim3(kNormNT), 0, st, static_cast<const TX *>(a.x), a.ldx, a.n, a.d, a.w,
                      a.b, (float)a.eps, static_cast<TY *>(a.y), a.ldy, a.mean,
                      a.rstd);
 }

@@ -41,6 +41,10 @@ ENTRY_POINTS = (
     "ezsp_knn_walk_stats",
     "ezsp_layer_norm", "ezsp_layer_norm_backward_workspace_size",
     "ezsp_layer_norm_backward",
+    "ezsp_linear_workspace_size", "ezsp_linear",
+    "ezsp_linear_backward_workspace_size", "ezsp_linear_backward",
+    "ezsp_gated_ff_workspace_size", "ezsp_gated_ff",
+    "ezsp_gated_ff_backward_workspace_size", "ezsp_gated_ff_backward",
 )
 
 
@@ -124,6 +128,22 @@ def load() -> ctypes.CDLL:
         "ezsp_layer_norm_backward": (ctypes.c_int, [
             P, i64, i32, P, i64, i32, i64, i32, P, P, P, P, i64, P, i64, P, P,
             P, sz, P]),
+        "ezsp_linear_workspace_size": (sz, [i64, i32, i32]),
+        "ezsp_linear": (ctypes.c_int, [P, i64, i64, i32, i32, i32, P, P, i32,
+                                       P, i64, P, i64, i32, P, i64, P, sz,
+                                       P]),
+        "ezsp_linear_backward_workspace_size": (sz, [i64, i32, i32, i32]),
+        "ezsp_linear_backward": (ctypes.c_int, [
+            P, i64, i32, P, i64, i64, i32, i32, i32, P, P, i64, i32, P, i64,
+            P, P, P, sz, P]),
+        "ezsp_gated_ff_workspace_size": (sz, [i64, i32, i32]),
+        "ezsp_gated_ff": (ctypes.c_int, [P, i64, i64, i32, i32, i32, P, P, P,
+                                         P, i32, P, i64, P, P, i64, P, sz,
+                                         P]),
+        "ezsp_gated_ff_backward_workspace_size": (sz, [i64, i32, i32, i32]),
+        "ezsp_gated_ff_backward": (ctypes.c_int, [
+            P, i64, P, i64, i64, i32, i32, i32, P, P, P, P, i64, i32, P, i64,
+            P, P, P, P, P, sz, P]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -154,7 +174,7 @@ def profile_only(stage=None):
 STAGES = ("morton_sort", "knn_query", "graph_build", "select", "union",
           "stats", "contract", "compose", "tail", "link")
 EXTRA_STAGES = ("grid_subsample", "edge_loss", "purity", "embed_mlp",
-                "layer_norm")
+                "layer_norm", "linear", "gated_ff")
 
 
 def profile_read(stage: str):
@@ -593,3 +613,160 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor,
         _at(dres), lddres, _at(dx), d, _at(dw), _at(db), ws.data_ptr(),
         nbytes, _stream(dev)), "ezsp_layer_norm_backward")
     return dx, dw, db
+
+
+def _weight(t, d_in, dtype, name, d_out=None):
+    """A contiguous device matrix [d_in, d_out] of the given type."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a device tensor")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != 2 or t.shape[0] != d_in or \
+            (d_out is not None and t.shape[1] != d_out):
+        raise ValueError(f"{name} must have shape [{d_in}, "
+                         f"{'d_out' if d_out is None else d_out}]")
+    return t.contiguous()
+
+
+def _act(act):
+    if act not in ACT_CODES:
+        raise ValueError(f"act must be one of {sorted(ACT_CODES)}")
+    return ACT_CODES[act]
+
+
+def linear(x: torch.Tensor, w: torch.Tensor, bias=None, act: str = "none",
+           residual=None, out_dtype=None, want_z: bool = False):
+    """y = act(x w + bias) + residual (ezsp_linear): x [n, d_in] and
+    w [d_in, d_out] bfloat16 or fp32, bias [d_out] fp32, residual [n, d_out]
+    of y's type, which is out_dtype (x's by default, or fp32).  act: none,
+    relu, gelu, silu.  Returns y, or with want_z (y, x w + bias) for
+    linear_backward.  Computed in stream order."""
+    lib = load()
+    x, ldx = _rows(x, "x")
+    n, d_in = x.shape
+    ty, dev = x.dtype, x.device
+    w = _weight(w, d_in, ty, "w")
+    d_out = w.shape[1]
+    code = _act(act)
+    bias = _vector(bias, d_out, "bias")
+    out_dtype = out_dtype or ty
+    if out_dtype not in (ty, torch.float32):
+        raise TypeError("out_dtype must be x's type or float32")
+    ldr = 0
+    if residual is not None:
+        residual, ldr = _rows(residual, "residual", n, d_out, out_dtype)
+    y = torch.empty((n, d_out), dtype=out_dtype, device=dev)
+    z = torch.empty((n, d_out), dtype=ty, device=dev) if want_z else None
+    nbytes = lib.ezsp_linear_workspace_size(n, d_in, d_out)
+    ws = _workspace(nbytes, dev)
+    _check(lib.ezsp_linear(
+        x.data_ptr(), ldx, n, d_in, d_out, TYPE_CODES[ty], w.data_ptr(),
+        _at(bias), code, _at(residual), ldr, y.data_ptr(), d_out,
+        TYPE_CODES[out_dtype], _at(z), d_out, ws.data_ptr(), nbytes,
+        _stream(dev)), "ezsp_linear")
+    return (y, z) if want_z else y
+
+
+def linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor,
+                    z=None, act: str = "none", want_dx: bool = True,
+                    want_dw: bool = True, want_db: bool = True):
+    """Gradients of linear (ezsp_linear_backward): (dx, dw of x's type,
+    dbias fp32), each None where it is not wanted.  dy [n, d_out] has x's
+    type or fp32; z is linear's second result (not needed without an
+    activation)."""
+    lib = load()
+    x, ldx = _rows(x, "x")
+    n, d_in = x.shape
+    ty, dev = x.dtype, x.device
+    w = _weight(w, d_in, ty, "w")
+    d_out = w.shape[1]
+    code = _act(act)
+    dy, lddy = _rows(dy, "dy", n, d_out)
+    ldz = 0
+    if z is not None:
+        z, ldz = _rows(z, "z", n, d_out, ty)
+    dx = torch.empty((n, d_in), dtype=ty, device=dev) if want_dx else None
+    dw = torch.empty((d_in, d_out), dtype=ty, device=dev) if want_dw else None
+    db = torch.empty(d_out, dtype=torch.float32, device=dev) \
+        if want_db else None
+    nbytes = lib.ezsp_linear_backward_workspace_size(n, d_in, d_out,
+                                                     TYPE_CODES[ty])
+    ws = _workspace(nbytes, dev)
+    _check(lib.ezsp_linear_backward(
+        dy.data_ptr(), lddy, TYPE_CODES[dy.dtype], x.data_ptr(), ldx, n, d_in,
+        d_out, TYPE_CODES[ty], w.data_ptr(), _at(z), ldz, code, _at(dx), d_in,
+        _at(dw), _at(db), ws.data_ptr(), nbytes, _stream(dev)),
+        "ezsp_linear_backward")
+    return dx, dw, db
+
+
+def gated_ff(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor,
+             b_gate=None, b_up=None, act: str = "silu",
+             want_saved: bool = False):
+    """h = act(x w_gate + b_gate) * (x w_up + b_up) in one kernel
+    (ezsp_gated_ff): x [n, d_in], weights [d_in, d_out], bfloat16 or fp32,
+    biases [d_out] fp32 or None.  Returns h, or with want_saved (h, gate,
+    up), the two sums that gated_ff_backward reads.  Computed in stream
+    order."""
+    lib = load()
+    x, ldx = _rows(x, "x")
+    n, d_in = x.shape
+    ty, dev = x.dtype, x.device
+    w_gate = _weight(w_gate, d_in, ty, "w_gate")
+    d_out = w_gate.shape[1]
+    w_up = _weight(w_up, d_in, ty, "w_up", d_out)
+    code = _act(act)
+    b_gate = _vector(b_gate, d_out, "b_gate")
+    b_up = _vector(b_up, d_out, "b_up")
+    h = torch.empty((n, d_out), dtype=ty, device=dev)
+    gate = up = None
+    if want_saved:
+        gate, up = torch.empty_like(h), torch.empty_like(h)
+    nbytes = lib.ezsp_gated_ff_workspace_size(n, d_in, d_out)
+    ws = _workspace(nbytes, dev)
+    _check(lib.ezsp_gated_ff(
+        x.data_ptr(), ldx, n, d_in, d_out, TYPE_CODES[ty], w_gate.data_ptr(),
+        _at(b_gate), w_up.data_ptr(), _at(b_up), code, h.data_ptr(), d_out,
+        _at(gate), _at(up), d_out, ws.data_ptr(), nbytes, _stream(dev)),
+        "ezsp_gated_ff")
+    return (h, gate, up) if want_saved else h
+
+
+def gated_ff_backward(dh: torch.Tensor, x: torch.Tensor,
+                      w_gate: torch.Tensor, w_up: torch.Tensor,
+                      gate: torch.Tensor, up: torch.Tensor,
+                      act: str = "silu", want_dx: bool = True,
+                      want_dw: bool = True, want_db: bool = True):
+    """Gradients of gated_ff (ezsp_gated_ff_backward): (dx, dw_gate, dw_up of
+    x's type, db_gate, db_up fp32), None where not wanted; gate and up are
+    gated_ff's saved sums."""
+    lib = load()
+    x, ldx = _rows(x, "x")
+    n, d_in = x.shape
+    ty, dev = x.dtype, x.device
+    w_gate = _weight(w_gate, d_in, ty, "w_gate")
+    d_out = w_gate.shape[1]
+    w_up = _weight(w_up, d_in, ty, "w_up", d_out)
+    code = _act(act)
+    dh, lddh = _rows(dh, "dh", n, d_out, ty)
+    gate, lds = _rows(gate, "gate", n, d_out, ty)
+    up, lds_up = _rows(up, "up", n, d_out, ty)
+    if lds != lds_up:
+        gate, up, lds = gate.contiguous(), up.contiguous(), d_out
+    dx = torch.empty((n, d_in), dtype=ty, device=dev) if want_dx else None
+    dwg = dwu = dbg = dbu = None
+    if want_dw:
+        dwg, dwu = torch.empty_like(w_gate), torch.empty_like(w_up)
+    if want_db:
+        dbg = torch.empty(d_out, dtype=torch.float32, device=dev)
+        dbu = torch.empty(d_out, dtype=torch.float32, device=dev)
+    nbytes = lib.ezsp_gated_ff_backward_workspace_size(n, d_in, d_out,
+                                                       TYPE_CODES[ty])
+    ws = _workspace(nbytes, dev)
+    _check(lib.ezsp_gated_ff_backward(
+        dh.data_ptr(), lddh, x.data_ptr(), ldx, n, d_in, d_out,
+        TYPE_CODES[ty], w_gate.data_ptr(), w_up.data_ptr(), gate.data_ptr(),
+        up.data_ptr(), lds, code, _at(dx), d_in, _at(dwg), _at(dwu),
+        _at(dbg), _at(dbu), ws.data_ptr(), nbytes, _stream(dev)),
+        "ezsp_gated_ff_backward")
+    return dx, dwg, dwu, dbg, dbu
