@@ -6,8 +6,8 @@
 //   dx = dg Wg^T + du Wu^T,  dWg = x^T dg,  dWu = x^T du,  db = row sums.
 // dg and du are formed once, side by side in one table; dx sums over both in
 // one product of twice the length, and both weights' gradients come from one
-// pass over x.
-#include "ezsp_gemm.h"
+// pass over x.  Few columns take the one-pass kernel instead.
+#include "ezsp_narrow.h"
 
 namespace ezsp {
 
@@ -25,8 +25,10 @@ struct PrepGated {
     const f32x8_t d = load8(dh + row * lddh + col, cnt);
     const f32x8_t g = load8(gate + row * lds + col, cnt);
     const f32x8_t u = load8(up + row * lds + col, cnt);
-    v[0] = d * u * act_grad8(g, act);
-    v[1] = d * act8(g, act);
+    f32x8_t a, da;
+    act_both8(g, act, a, da);
+    v[0] = d * u * da;
+    v[1] = d * a;
   }
   __device__ __forceinline__ void put(int64_t row, int32_t col, int32_t cnt,
                                       const f32x8_t *v) const {
@@ -35,6 +37,67 @@ struct PrepGated {
     store8(dz + row * lddz + half + col, v[1], cnt);
   }
 };
+
+// The same for the one-pass backward: dg and du from registers.
+struct NarrowGated {
+  const __bf16 *dh, *gate, *up;
+  int64_t lddh, lds;
+  int32_t act;
+  struct Raw {
+    Vec8<__bf16> d, g, u;
+  };
+  __device__ __forceinline__ Raw raw(int64_t row, int32_t n, int32_t d,
+                                     Span s) const {
+    Raw r;
+    int32_t back;
+    r.d = raw8(dh + span_at<__bf16>(row, lddh, n, d, s, back));
+    const int64_t at = span_at<__bf16>(row, lds, n, d, s, back);
+    r.g = raw8(gate + at);
+    r.u = raw8(up + at);
+    return r;
+  }
+  __device__ __forceinline__ void value(const Raw &r, int64_t row, int32_t n,
+                                        int32_t d, Span s, f32x8_t *v) const {
+    const int32_t cnt = row < n ? s.cnt : 0;
+    int32_t back;
+    span_at<__bf16>(row, lds, n, d, s, back);
+    const f32x8_t g =
+        __builtin_convertvector(settle(r.g, s.off + back, cnt), f32x8_t);
+    const f32x8_t u =
+        __builtin_convertvector(settle(r.u, s.off + back, cnt), f32x8_t);
+    span_at<__bf16>(row, lddh, n, d, s, back);
+    const f32x8_t dv =
+        __builtin_convertvector(settle(r.d, s.off + back, cnt), f32x8_t);
+    f32x8_t a, da;
+    act_both8(g, act, a, da);
+    v[0] = dv * u * da;
+    v[1] = dv * a;
+  }
+};
+
+void backward_narrow(const GatedArgs &a, hipStream_t st) {
+  NarrowArgs g = {};
+  g.x = static_cast<const __bf16 *>(a.x);
+  g.w[0] = static_cast<const __bf16 *>(a.w_gate);
+  g.w[1] = static_cast<const __bf16 *>(a.w_up);
+  g.ldx = a.ldx;
+  g.n = a.n;
+  g.d_in = a.d_in;
+  g.d_out = a.d_out;
+  g.dx = static_cast<__bf16 *>(a.dx);
+  g.lddx = a.lddx;
+  g.part = a.part;
+  NarrowGated op;
+  op.dh = static_cast<const __bf16 *>(a.dh);
+  op.gate = static_cast<const __bf16 *>(a.gate);
+  op.up = static_cast<const __bf16 *>(a.up);
+  op.lddh = a.lddh;
+  op.lds = a.lds;
+  op.act = a.act;
+  narrow<NarrowGated, 2>(g, op, static_cast<__bf16 *>(a.dw_gate),
+                         static_cast<__bf16 *>(a.dw_up), a.db_gate, a.db_up,
+                         st);
+}
 
 template <class T>
 void forward(const GatedArgs &a, hipStream_t st) {
@@ -62,6 +125,12 @@ void forward(const GatedArgs &a, hipStream_t st) {
 
 template <class T>
 void backward(const GatedArgs &a, hipStream_t st) {
+  if constexpr (sizeof(T) == 2) {
+    if (narrow_fits(a.n, a.d_in, a.d_out, 2)) {
+      backward_narrow(a, st);
+      return;
+    }
+  }
   const int64_t half = pad_row(a.d_out);
   T *dz = static_cast<T *>(a.dz);
   {
@@ -118,11 +187,17 @@ void gated_reserve(Arena &ar, int64_t n, int64_t d_in, int64_t d_out,
                    int32_t type, bool bwd, GatedArgs *a) {
   a->part_bytes = gemm_part_bytes(d_in, n, d_out, 2);
   if (bwd) {
-    a->part_bytes =
-        std::max(gemm_part_bytes(2 * d_out, n, d_in, 1),
-                 std::max(gemm_part_bytes(n, d_in, d_out, 2),
-                          (size_t)prep_parts(n) * 2 * (size_t)d_out * 4));
-    a->dz = ar.take<char>((size_t)n * 2 * (size_t)pad_row(d_out) *
+    // (sizes may not fall where the one-pass kernel starts to serve)
+    const int64_t rows = type == EZSP_TYPE_BF16 && narrow_fits(n, d_in, d_out, 2)
+                             ? kVec - 1
+                             : n;
+    a->part_bytes = std::max(
+        std::max(narrow_part_bytes(n, std::min<int64_t>(d_in, 128),
+                                   std::min<int64_t>(d_out, 512), 2),
+                 (size_t)prep_parts(rows) * 2 * (size_t)d_out * 4),
+        std::max(gemm_part_bytes(2 * d_out, rows, d_in, 1),
+                 gemm_part_bytes(rows, d_in, d_out, 2)));
+    a->dz = ar.take<char>((size_t)rows * 2 * (size_t)pad_row(d_out) *
                           type_bytes(type));
   }
   a->part = reinterpret_cast<float *>(ar.take<char>(a->part_bytes));

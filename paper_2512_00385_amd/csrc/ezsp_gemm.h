@@ -8,8 +8,9 @@
 // into LDS as they lie in memory, 128 bytes of k at a time (64 bfloat16, 32
 // fp32 values):
 //   K-major  rows of 128 bytes, read as 16-byte pieces along k; piece p of
-//            row r sits at p ^ (r mod 8), so that the 32 rows of a fragment
-//            spread over the banks;
+//            row r sits at p ^ (r / 2 mod 8): two rows fill the 64 banks
+//            once, and 16 rows read without a conflict (with r mod 8 every
+//            second access was one);
 //   else     one line per k, read through ds_read_b64_tr_b16, which hands
 //            every lane four consecutive k of its own column (fp32: four
 //            separate reads).  A line's 64-byte pieces are exchanged by the
@@ -58,13 +59,20 @@ __device__ __forceinline__ uint32_t lds_addr(const void *lds) {
   return (uint32_t)(uintptr_t)(
       (const __attribute__((address_space(3))) void *)lds);
 }
+// A pointer that is the same in every lane, where the compiler can't tell.
+__device__ __forceinline__ const void *uniform(const void *p) {
+  const uint64_t v = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v);
+  const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)(v >> 32));
+  return reinterpret_cast<const void *>(((uint64_t)hi << 32) | lo);
+}
 __device__ __forceinline__ void copy_to_lds16(const void *base, uint32_t off,
                                               uint32_t lds) {
   asm volatile(
       "s_mov_b32 m0, %0\n\ts_nop 0\n\t"
       "global_load_lds_dwordx4 %1, %2"
       :
-      : "s"(lds), "v"(off), "s"(base)
+      : "s"(lds), "v"(off), "s"(uniform(base))
       : "memory", "m0");
 }
 __device__ __forceinline__ void copy_to_lds16(const void *src, uint32_t lds) {
@@ -85,6 +93,7 @@ __device__ __forceinline__ void copies_landed() {
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 typedef short s16x8_t __attribute__((ext_vector_type(8)));
 
+constexpr int64_t kCus = 256;    // of an MI355X
 constexpr int kLineBytes = 128;  // bytes of k in an LDS tile
 
 // One operand's LDS tile: R rows (its own index) by 128 bytes of k.
@@ -113,7 +122,7 @@ struct Tile {
     const int c = i * NT + (int)threadIdx.x;
     if constexpr (KMAJOR) {
       r = c >> 3;
-      k = ((c & 7) ^ (r & 7)) * kPer;
+      k = ((c & 7) ^ ((r >> 1) & 7)) * kPer;
     } else {
       k = c / kLine;
       r = ((c % kLine) ^ line_swz(k)) * kPer;
@@ -211,7 +220,7 @@ struct Tile {
   static __device__ __forceinline__ u32x4_t frag(const char *lds, int row0,
                                                  int s, int lane) {
     if constexpr (KMAJOR) {
-      const int piece = (2 * s + (lane >> 5)) ^ (lane & 7);
+      const int piece = (2 * s + (lane >> 5)) ^ ((lane >> 1) & 7);
       return *reinterpret_cast<const u32x4_t *>(
           lds + (row0 + (lane & 31)) * kLineBytes + piece * 16);
     } else if constexpr (sizeof(T) == 2) {
@@ -276,7 +285,9 @@ struct Shape {
   // epilogue: 32 rows of a wave's columns
   static constexpr int kOutLd = TN * 32 + 4;
   static constexpr int kOut = 32 * kOutLd * 4;
-  static_assert(WM * WN * kOut <= 2 * kStage, "epilogue fits the stages");
+  // waves whose part fits one stage; the others' lie past both
+  static constexpr int kFit = kStage / kOut < WM * WN ? kStage / kOut : WM * WN;
+  static constexpr int kLds = 2 * kStage + (WM * WN - kFit) * kOut;
 };
 
 // Logical tile of block b out of total: XCD x takes the x-th contiguous run
@@ -300,101 +311,141 @@ __device__ __forceinline__ void tile_of(int32_t b, int32_t total,
   tn = in / rows;
 }
 
+// A block takes tiles of D gridDim.x apart and keeps one pipeline running
+// across them.  Its steps are LDS tiles of k; while one is multiplied,
+//  - the next one lies in LDS or lands there (FAST: two steps ahead, issued as
+//    soon as its stage is free; else one, by way of registers),
+//  - each quarter's fragments are read while the quarter before is
+//    multiplied, the next step's first ones during the last quarter, so that
+//    the barrier between two steps has multiplications to hide behind.
+// During an epilogue the next tile's first step is on its way.
 template <class S, class Epi>
 __global__ __launch_bounds__(S::NT) void k_gemm(GemmArgs<typename S::T> g,
                                                 Epi epi) {
   typedef typename S::T T;
-  __shared__ __attribute__((aligned(16))) char stages[2 * S::kStage];
+  __shared__ __attribute__((aligned(16))) char stages[S::kLds];
   const int lane = threadIdx.x & (kWave - 1);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int wm = wave / S::WN, wn = wave % S::WN;
   const int32_t total = g.tiles_m * g.tiles_n * g.splits;
-  const int32_t kt1 = (g.k + S::kK - 1) / S::kK;  // LDS tiles of one pair
+  const int32_t kt1 = (g.k + S::kK - 1) / S::kK;  // steps of one pair
   const int32_t kt_all = S::MODE == kSeq ? 2 * kt1 : kt1;
 
-  for (int32_t blk = blockIdx.x; blk < total; blk += gridDim.x) {
+  // the tile and step to fetch next
+  typename S::TileA ta;
+  typename S::TileB tb[S::NB];
+  int32_t f_blk = blockIdx.x, m0 = 0, n0 = 0, f_t = 0, f_end = 0;
+  auto open = [&] {
     int32_t tm, tn, sp;
-    tile_of(blk, total, g.tiles_m, g.tiles_n, tm, tn, sp);
-    const int32_t m0 = tm * S::BM, n0 = tn * S::CN;
-    const int32_t t_begin = sp * g.kt_split;
-    const int32_t t_end = min(kt_all, t_begin + g.kt_split);
-    typename S::TileA ta;
-    typename S::TileB tb[S::NB];
+    tile_of(f_blk, total, g.tiles_m, g.tiles_n, tm, tn, sp);
+    m0 = tm * S::BM;
+    n0 = tn * S::CN;
+    f_t = sp * g.kt_split;
+    f_end = min(kt_all, f_t + g.kt_split);
     ta.init(g.m - m0, g.lda);
 #pragma unroll
     for (int p = 0; p < S::NB; ++p) tb[p].init(g.n - n0, g.ldb);
-
-    auto fetch = [&](int32_t t, char *st) {
-      const bool second = S::MODE == kSeq && t >= kt1;
-      const int32_t k0 = (second ? t - kt1 : t) * S::kK;
-      const T *a = second ? g.a[1] : g.a[0];
-      ta.fetch(S::AK ? a + (int64_t)m0 * g.lda + k0
-                     : a + (int64_t)k0 * g.lda + m0,
-               g.lda, g.m - m0, g.k - k0, st);
+  };
+  auto fetch = [&](char *st) {
+    if (f_blk >= total) return;
+    const bool second = S::MODE == kSeq && f_t >= kt1;
+    const int32_t k0 = (second ? f_t - kt1 : f_t) * S::kK;
+    const T *a = second ? g.a[1] : g.a[0];
+    ta.fetch(S::AK ? a + (int64_t)m0 * g.lda + k0
+                   : a + (int64_t)k0 * g.lda + m0,
+             g.lda, g.m - m0, g.k - k0, st);
 #pragma unroll
-      for (int p = 0; p < S::NB; ++p) {
-        const T *b = (second || p) ? g.b[1] : g.b[0];
-        tb[p].fetch(S::BK ? b + (int64_t)n0 * g.ldb + k0
-                          : b + (int64_t)k0 * g.ldb + n0,
-                    g.ldb, g.n - n0, g.k - k0,
-                    st + S::TileA::kBytes + p * S::TileB::kBytes);
-      }
-    };
-    auto put = [&](char *st) {
-      ta.put(st);
+    for (int p = 0; p < S::NB; ++p) {
+      const T *b = (second || p) ? g.b[1] : g.b[0];
+      tb[p].fetch(S::BK ? b + (int64_t)n0 * g.ldb + k0
+                        : b + (int64_t)k0 * g.ldb + n0,
+                  g.ldb, g.n - n0, g.k - k0,
+                  st + S::TileA::kBytes + p * S::TileB::kBytes);
+    }
+    if (++f_t == f_end) {
+      f_blk += gridDim.x;
+      if (f_blk < total) open();
+    }
+  };
+  auto put = [&](char *st) {
+    ta.put(st);
 #pragma unroll
-      for (int p = 0; p < S::NB; ++p)
-        tb[p].put(st + S::TileA::kBytes + p * S::TileB::kBytes);
-    };
+    for (int p = 0; p < S::NB; ++p)
+      tb[p].put(st + S::TileA::kBytes + p * S::TileB::kBytes);
+  };
 
-    f32x16_t acc[S::TM][S::TN];
+  f32x16_t acc[S::TM][S::TN];
+  u32x4_t fa[2][S::TM], fb[2][S::TN];  // fragments of quarters, in turn
+  auto frags = [&](const char *st, int s) {
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i)
+      fa[s & 1][i] = S::TileA::frag(st, (wm * S::TM + i) * 32, s, lane);
+#pragma unroll
+    for (int j = 0; j < S::TN; ++j) {
+      const int p = j / (S::TN / S::NB), jj = j % (S::TN / S::NB);
+      fb[s & 1][j] =
+          S::TileB::frag(st + S::TileA::kBytes + p * S::TileB::kBytes,
+                         wn * S::WC + jj * 32, s, lane);
+    }
+  };
+  auto multiply = [&](int s) {
+#pragma unroll
+    for (int i = 0; i < S::TM; ++i)
+#pragma unroll
+      for (int j = 0; j < S::TN; ++j)
+        acc[i][j] = mma<T>(fb[s & 1][j], fa[s & 1][i], acc[i][j]);
+  };
+
+  int32_t blk = blockIdx.x;
+  if (blk >= total) return;
+  int32_t cur = 0;  // the stage being multiplied
+  open();
+  fetch(stages);
+  put(stages);
+  if (S::FAST) fetch(stages + S::kStage);
+  copies_landed();
+  __syncthreads();
+  frags(stages, 0);
+  while (true) {
+    int32_t tm, tn, tile_sp;
+    tile_of(blk, total, g.tiles_m, g.tiles_n, tm, tn, tile_sp);
+    const int32_t tile_m0 = tm * S::BM, tile_n0 = tn * S::CN;
+    const int32_t steps =
+        min(kt_all - tile_sp * g.kt_split, g.kt_split);
+    blk += gridDim.x;
+    const bool more = blk < total;
 #pragma unroll
     for (int i = 0; i < S::TM; ++i)
 #pragma unroll
       for (int j = 0; j < S::TN; ++j) acc[i][j] = f32x16_t(0.0f);
-
-    auto compute = [&](const char *st) {
+    for (int32_t t = 0; t < steps; ++t) {
+      char *here = stages + cur, *next = stages + (S::kStage - cur);
+      const bool ahead = t + 1 < steps || more;
+      if (!S::FAST && ahead) fetch(next);
 #pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        u32x4_t fa[S::TM], fb[S::TN];
-#pragma unroll
-        for (int i = 0; i < S::TM; ++i)
-          fa[i] = S::TileA::frag(st, (wm * S::TM + i) * 32, s, lane);
-#pragma unroll
-        for (int j = 0; j < S::TN; ++j) {
-          const int p = j / (S::TN / S::NB), jj = j % (S::TN / S::NB);
-          fb[j] = S::TileB::frag(
-              st + S::TileA::kBytes + p * S::TileB::kBytes,
-              wn * S::WC + jj * 32, s, lane);
-        }
-#pragma unroll
-        for (int i = 0; i < S::TM; ++i)
-#pragma unroll
-          for (int j = 0; j < S::TN; ++j)
-            acc[i][j] = mma<T>(fb[j], fa[i], acc[i][j]);
+      for (int s = 0; s < 3; ++s) {
+        frags(here, s + 1);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(s);
       }
-    };
-
-    int32_t cur = 0;
-    fetch(t_begin, stages);
-    put(stages);
-    copies_landed();
-    __syncthreads();
-    for (int32_t t = t_begin; t < t_end; ++t) {
-      char *next = stages + (S::kStage - cur);
-      if (t + 1 < t_end) fetch(t + 1, next);
-      compute(stages + cur);
-      if (t + 1 < t_end) put(next);
+      if (!S::FAST && ahead) put(next);
       copies_landed();
       __syncthreads();
+      if (S::FAST && t + 1 < steps) fetch(here);
+      frags(next, 0);  // (of no use after a block's last step)
+      __builtin_amdgcn_sched_barrier(0);
+      multiply(3);
       cur = S::kStage - cur;
     }
 
-    // epilogue: 32 rows at a time through the wave's own part of LDS, so
-    // that each lane ends up with kVec neighbouring columns of a row
-    float *out = reinterpret_cast<float *>(stages + wave * S::kOut);
+    // epilogue: 32 rows at a time through the wave's own part of LDS (the
+    // stage just read, and what lies past both), so that each lane ends up
+    // with kVec neighbouring columns of a row
+    float *out = reinterpret_cast<float *>(
+        stages + (wave < S::kFit ? S::kStage - cur + wave * S::kOut
+                                 : 2 * S::kStage + (wave - S::kFit) * S::kOut));
     constexpr int kLanes = S::WC / kVec;  // lanes of a row
-    const int32_t col = n0 + wn * S::WC + (lane % kLanes) * kVec;
+    const int32_t col = tile_n0 + wn * S::WC + (lane % kLanes) * kVec;
 #pragma unroll
     for (int i = 0; i < S::TM; ++i) {
 #pragma unroll
@@ -411,7 +462,7 @@ __global__ __launch_bounds__(S::NT) void k_gemm(GemmArgs<typename S::T> g,
 #pragma unroll
       for (int pass = 0; pass < 32 * kLanes / kWave; ++pass) {
         const int r = pass * (kWave / kLanes) + lane / kLanes;
-        const int32_t row = m0 + (wm * S::TM + i) * 32 + r;
+        const int32_t row = tile_m0 + (wm * S::TM + i) * 32 + r;
         const float *src = out + r * S::kOutLd + (lane % kLanes) * kVec;
         f32x8_t v[S::NB];
 #pragma unroll
@@ -426,12 +477,14 @@ __global__ __launch_bounds__(S::NT) void k_gemm(GemmArgs<typename S::T> g,
           if (g.splits == 1)
             epi.apply(row, col, g.n - col, v);
           else
-            epi.partial(sp, g.m, g.n, row, col, v);
+            epi.partial(tile_sp, g.m, g.n, row, col, v);
         }
       }
       __builtin_amdgcn_wave_barrier();
     }
-    __syncthreads();  // the stages are free again
+    if (!more) break;
+    __syncthreads();  // the other stage is free again
+    if (S::FAST) fetch(stages + (S::kStage - cur));
   }
 }
 
@@ -540,8 +593,17 @@ void gemm_launch(GemmArgs<typename S::T> g, const Epi &epi, int32_t splits,
   g.kt_split = (kt + splits - 1) / splits;
   g.splits = (kt + g.kt_split - 1) / g.kt_split;  // no empty part
   const int64_t total = (int64_t)g.tiles_m * g.tiles_n * g.splits;
+  // as many blocks as the chip holds at once
+  static const int64_t slots = [] {
+    int per_cu = 0;
+    if (hipOccupancyMaxActiveBlocksPerMultiprocessor(
+            &per_cu, (const void *)k_gemm<S, Epi>, S::NT, 0) != hipSuccess ||
+        per_cu < 1)
+      per_cu = 1;
+    return (int64_t)per_cu * kCus;
+  }();
   hipLaunchKernelGGL((k_gemm<S, Epi>),
-                     dim3((unsigned)std::min<int64_t>(total, 1 << 21)),
+                     dim3((unsigned)std::min<int64_t>(total, slots)),
                      dim3(S::NT), 0, st, g, epi);
   if (g.splits > 1) {
     const int64_t items = (int64_t)g.m * ((g.n + kVec - 1) / kVec);

@@ -3,8 +3,9 @@
 // The forward pass is one matrix product with everything else in its
 // epilogue.  Backward, dz is formed once (both products read it) with the
 // bias's sums on the way; for bfloat16 it is rounded there, since the matrix
-// cores take it so, while db is summed from the unrounded values.
-#include "ezsp_gemm.h"
+// cores take it so, while db is summed from the unrounded values.  Few
+// columns take the one-pass kernel instead.
+#include "ezsp_narrow.h"
 
 namespace ezsp {
 
@@ -31,6 +32,64 @@ struct PrepLinear {
     if (dz) store8(dz + row * lddz + col, v[0], cnt);
   }
 };
+
+// The same for the one-pass backward (bfloat16): dz from registers.
+template <class TY, bool ACT>
+struct NarrowLinear {
+  const TY *dy;
+  int64_t lddy;
+  const __bf16 *z;
+  int64_t ldz;
+  int32_t act;
+  struct Raw {
+    Vec8<TY> dy;
+    Vec8<__bf16> z[ACT ? 1 : 0];
+  };
+  __device__ __forceinline__ Raw raw(int64_t row, int32_t n, int32_t d,
+                                     Span s) const {
+    Raw r;
+    int32_t back;
+    r.dy = raw8(dy + span_at<TY>(row, lddy, n, d, s, back));
+    if constexpr (ACT)
+      r.z[0] = raw8(z + span_at<__bf16>(row, ldz, n, d, s, back));
+    return r;
+  }
+  __device__ __forceinline__ void value(const Raw &r, int64_t row, int32_t n,
+                                        int32_t d, Span s, f32x8_t *v) const {
+    const int32_t cnt = row < n ? s.cnt : 0;
+    int32_t back;
+    span_at<TY>(row, lddy, n, d, s, back);
+    v[0] = __builtin_convertvector(settle(r.dy, s.off + back, cnt), f32x8_t);
+    if constexpr (ACT) {
+      span_at<__bf16>(row, ldz, n, d, s, back);
+      v[0] *= act_grad8(__builtin_convertvector(
+                            settle(r.z[0], s.off + back, cnt), f32x8_t),
+                        act);
+    }
+  }
+};
+
+template <class TY, bool ACT>
+void backward_narrow(const LinearArgs &a, hipStream_t st) {
+  NarrowArgs g = {};
+  g.x = static_cast<const __bf16 *>(a.x);
+  g.w[0] = g.w[1] = static_cast<const __bf16 *>(a.w);
+  g.ldx = a.ldx;
+  g.n = a.n;
+  g.d_in = a.d_in;
+  g.d_out = a.d_out;
+  g.dx = static_cast<__bf16 *>(a.dx);
+  g.lddx = a.lddx;
+  g.part = a.part;
+  NarrowLinear<TY, ACT> op;
+  op.dy = static_cast<const TY *>(a.dy);
+  op.lddy = a.lddy;
+  op.z = static_cast<const __bf16 *>(a.z);
+  op.ldz = a.ldz;
+  op.act = a.act;
+  narrow<NarrowLinear<TY, ACT>, 1>(g, op, static_cast<__bf16 *>(a.dw),
+                                   nullptr, a.db, nullptr, st);
+}
 
 // dz has to be formed unless dy is it already
 bool needs_dz(const LinearArgs &a) {
@@ -64,6 +123,18 @@ void forward(const LinearArgs &a, hipStream_t st) {
 
 template <class T>
 void backward(const LinearArgs &a, hipStream_t st) {
+  if constexpr (sizeof(T) == 2) {
+    if (narrow_fits(a.n, a.d_in, a.d_out, 1)) {
+      const bool wide_y = a.type_y == EZSP_TYPE_F32;
+      if (a.act == EZSP_ACT_NONE)
+        wide_y ? backward_narrow<float, false>(a, st)
+               : backward_narrow<__bf16, false>(a, st);
+      else
+        wide_y ? backward_narrow<float, true>(a, st)
+               : backward_narrow<__bf16, true>(a, st);
+      return;
+    }
+  }
   const bool form = needs_dz(a) && (a.dx || a.dw);
   const T *dz = static_cast<const T *>(a.dy);
   int64_t lddz = a.lddy;
@@ -118,11 +189,18 @@ void linear_reserve(Arena &ar, int64_t n, int64_t d_in, int64_t d_out,
                     int32_t type, bool bwd, LinearArgs *a) {
   a->part_bytes = gemm_part_bytes(d_in, n, d_out, 1);
   if (bwd) {
-    a->part_bytes =
-        std::max(gemm_part_bytes(d_out, n, d_in, 1),
-                 std::max(gemm_part_bytes(n, d_in, d_out, 1),
-                          (size_t)prep_parts(n) * (size_t)d_out * 4));
-    a->dz = ar.take<char>((size_t)n * (size_t)pad_row(d_out) *
+    // the one-pass kernel needs its parts alone, but sizes may not fall where
+    // it starts to serve
+    const int64_t rows = type == EZSP_TYPE_BF16 && narrow_fits(n, d_in, d_out, 1)
+                             ? kVec - 1
+                             : n;
+    a->part_bytes = std::max(
+        std::max(narrow_part_bytes(n, std::min<int64_t>(d_in, 128),
+                                   std::min<int64_t>(d_out, 512), 1),
+                 (size_t)prep_parts(rows) * (size_t)d_out * 4),
+        std::max(gemm_part_bytes(d_out, rows, d_in, 1),
+                 gemm_part_bytes(rows, d_in, d_out, 1)));
+    a->dz = ar.take<char>((size_t)rows * (size_t)pad_row(d_out) *
                           type_bytes(type));
   }
   a->part = reinterpret_cast<float *>(ar.take<char>(a->part_bytes));

@@ -18,6 +18,10 @@ SIZES = [
     (129, 72, 136), (130, 4, 6), (257, 6, 32), (300, 515, 77), (500, 32, 65),
     (511, 136, 264), (1000, 33, 1), (1003, 32, 128), (2000, 24, 48),
     (4100, 64, 130),
+    # few columns: each split of the one-pass backward
+    (7, 12, 20), (8, 5, 3), (65, 31, 33), (700, 32, 40), (700, 20, 250),
+    (700, 60, 30), (700, 64, 64), (700, 57, 200), (700, 100, 30),
+    (700, 128, 64), (700, 97, 100), (20_000, 3, 7),
 ]
 EXACT = SIZES + [(4096, 64, 1600), (3333, 200, 2056), (70, 20_000, 40),
                  (20, 30_001, 9), (50_021, 16, 24)]

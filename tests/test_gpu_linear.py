@@ -19,6 +19,10 @@ SIZES = [
     (128, 64, 128), (129, 72, 136), (130, 4, 6), (257, 6, 32), (300, 515, 77),
     (500, 32, 65), (511, 136, 264), (1000, 33, 1), (1000, 1, 50),
     (1003, 128, 32), (2000, 24, 48), (4100, 64, 130),
+    # few columns: each split of the one-pass backward
+    (7, 12, 20), (8, 5, 3), (65, 31, 33), (700, 32, 128), (700, 20, 250),
+    (700, 30, 400), (700, 60, 64), (700, 64, 500), (700, 100, 30),
+    (700, 128, 100), (700, 97, 256), (20_000, 3, 7),
 ]
 
 
