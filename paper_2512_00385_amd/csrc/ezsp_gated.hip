@@ -7,6 +7,7 @@
 // dg and du are formed once, side by side in one table; dx sums over both in
 // one product of twice the length, and both weights' gradients come from one
 // pass over x.  Few columns take the one-pass kernel instead.
+#include "ezsp_few.h"
 #include "ezsp_narrow.h"
 
 namespace ezsp {
@@ -120,7 +121,10 @@ void forward(const GatedArgs &a, hipStream_t st) {
   e.up = static_cast<T *>(a.up);
   e.lds = a.lds;
   e.act = a.act;
-  gemm<T, true, false, kDual>(g, e, a.part_bytes, st);
+  if (few_serves(g, 2))
+    few<T, 2>(g, e, st);
+  else
+    gemm<T, true, false, kDual>(g, e, a.part_bytes, st);
 }
 
 template <class T>

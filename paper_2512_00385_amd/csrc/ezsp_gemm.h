@@ -488,26 +488,41 @@ __global__ __launch_bounds__(S::NT) void k_gemm(GemmArgs<typename S::T> g,
   }
 }
 
-// The parts of a split sum, added in order, through the epilogue.
+// The parts of a split sum, added in order, through the epilogue.  kJoinAhead
+// parts are loaded at once: one after the other, their latencies would cost
+// more than the product they end.
+constexpr int kJoinAhead = 8;
 template <int NB, class Epi>
-__global__ __launch_bounds__(256) void k_gemm_join(int32_t splits, int32_t m,
-                                                   int32_t n, Epi epi) {
+__global__ __launch_bounds__(64) void k_gemm_join(int32_t splits, int32_t m,
+                                                  int32_t n, Epi epi) {
   const int32_t per_row = (n + kVec - 1) / kVec;
   const int64_t items = (int64_t)m * per_row;
-  for (int64_t it = (int64_t)blockIdx.x * 256 + threadIdx.x; it < items;
-       it += (int64_t)gridDim.x * 256) {
+  const int64_t next = (int64_t)NB * m * n;  // from part to part
+  for (int64_t it = (int64_t)blockIdx.x * 64 + threadIdx.x; it < items;
+       it += (int64_t)gridDim.x * 64) {
     const int32_t row = (int32_t)(it / per_row);
     const int32_t col = (int32_t)(it % per_row) * kVec;
+    const int32_t cnt = n - col;
     f32x8_t v[NB];
 #pragma unroll
-    for (int p = 0; p < NB; ++p) v[p] = f32x8_t(0.0f);
-    for (int32_t s = 0; s < splits; ++s)
+    for (int p = 0; p < NB; ++p) {
+      const float *src = epi.part + ((int64_t)p * m + row) * n + col;
+      f32x8_t sum = f32x8_t(0.0f);
+      int32_t s = 0;
+      if (cnt >= kVec) {
+        for (; s + kJoinAhead <= splits; s += kJoinAhead) {
+          f32x8_t t[kJoinAhead];
 #pragma unroll
-      for (int p = 0; p < NB; ++p)
-        v[p] += load8(epi.part +
-                          (((int64_t)s * NB + p) * m + row) * n + col,
-                      n - col);
-    epi.apply(row, col, n - col, v);
+          for (int q = 0; q < kJoinAhead; ++q)
+            t[q] = *reinterpret_cast<const f32x8_u *>(src + (s + q) * next);
+#pragma unroll
+          for (int q = 0; q < kJoinAhead; ++q) sum += t[q];
+        }
+      }
+      for (; s < splits; ++s) sum += load8(src + s * next, cnt);
+      v[p] = sum;
+    }
+    epi.apply(row, col, cnt, v);
   }
 }
 
@@ -608,9 +623,9 @@ void gemm_launch(GemmArgs<typename S::T> g, const Epi &epi, int32_t splits,
   if (g.splits > 1) {
     const int64_t items = (int64_t)g.m * ((g.n + kVec - 1) / kVec);
     hipLaunchKernelGGL((k_gemm_join<S::NB, Epi>),
-                       dim3((unsigned)std::min<int64_t>((items + 255) / 256,
-                                                        1 << 16)),
-                       dim3(256), 0, st, g.splits, g.m, g.n, epi);
+                       dim3((unsigned)std::min<int64_t>((items + 63) / 64,
+                                                        1 << 18)),
+                       dim3(64), 0, st, g.splits, g.m, g.n, epi);
   }
 }
 

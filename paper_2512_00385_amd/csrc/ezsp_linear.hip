@@ -5,6 +5,7 @@
 // bias's sums on the way; for bfloat16 it is rounded there, since the matrix
 // cores take it so, while db is summed from the unrounded values.  Few
 // columns take the one-pass kernel instead.
+#include "ezsp_few.h"
 #include "ezsp_narrow.h"
 
 namespace ezsp {
@@ -118,7 +119,10 @@ void forward(const LinearArgs &a, hipStream_t st) {
   e.type = a.type;
   e.type_y = a.type_y;
   e.act = a.act;
-  gemm<T, true, false, kPlain>(g, e, a.part_bytes, st);
+  if (few_serves(g, 1))
+    few<T, 1>(g, e, st);
+  else
+    gemm<T, true, false, kPlain>(g, e, a.part_bytes, st);
 }
 
 template <class T>

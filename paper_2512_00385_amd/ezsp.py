@@ -9,6 +9,7 @@ library is missing, loading raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import numpy as np
@@ -558,6 +559,25 @@ def _at(t):
     return None if t is None else t.data_ptr()
 
 
+# The calls below may take less time on the GPU than their arguments on the
+# host, so their sizes are queried once each and the stream is read without
+# torch's Stream object.
+@functools.lru_cache(maxsize=4096)
+def _dense_bytes(name: str, *sizes) -> int:
+    nbytes = getattr(load(), name)(*sizes)
+    if nbytes == 0:
+        raise EzspError(ERR_INVALID_ARG, "workspace size", "invalid sizes")
+    return nbytes
+
+
+def _dense_ws(nbytes: int, device):
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 def layer_norm(x: torch.Tensor, weight=None, bias=None, eps: float = 1e-5,
                out_dtype=None, want_stats: bool = False):
     """Layer norm over each row of x [n, d] (ezsp_layer_norm), bfloat16 or
@@ -579,7 +599,7 @@ def layer_norm(x: torch.Tensor, weight=None, bias=None, eps: float = 1e-5,
     _check(lib.ezsp_layer_norm(
         x.data_ptr(), ldx, TYPE_CODES[x.dtype], n, d, _at(weight), _at(bias),
         float(eps), y.data_ptr(), d, TYPE_CODES[out_dtype], _at(mean),
-        _at(rstd), _stream(x.device)), "ezsp_layer_norm")
+        _at(rstd), _raw_stream(x.device.index)), "ezsp_layer_norm")
     return (y, mean, rstd) if want_stats else y
 
 
@@ -605,13 +625,13 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor,
     if want_sums:
         dw = torch.empty(d, dtype=torch.float32, device=dev)
         db = torch.empty(d, dtype=torch.float32, device=dev)
-    nbytes = lib.ezsp_layer_norm_backward_workspace_size(n, d)
-    ws = _workspace(nbytes, dev)
+    nbytes = _dense_bytes("ezsp_layer_norm_backward_workspace_size", n, d)
+    ws = _dense_ws(nbytes, dev)
     _check(lib.ezsp_layer_norm_backward(
         dy.data_ptr(), lddy, TYPE_CODES[dy.dtype], x.data_ptr(), ldx,
         TYPE_CODES[x.dtype], n, d, _at(weight), _at(mean), _at(rstd),
         _at(dres), lddres, _at(dx), d, _at(dw), _at(db), ws.data_ptr(),
-        nbytes, _stream(dev)), "ezsp_layer_norm_backward")
+        nbytes, _raw_stream(dev.index)), "ezsp_layer_norm_backward")
     return dx, dw, db
 
 
@@ -657,13 +677,13 @@ def linear(x: torch.Tensor, w: torch.Tensor, bias=None, act: str = "none",
         residual, ldr = _rows(residual, "residual", n, d_out, out_dtype)
     y = torch.empty((n, d_out), dtype=out_dtype, device=dev)
     z = torch.empty((n, d_out), dtype=ty, device=dev) if want_z else None
-    nbytes = lib.ezsp_linear_workspace_size(n, d_in, d_out)
-    ws = _workspace(nbytes, dev)
+    nbytes = _dense_bytes("ezsp_linear_workspace_size", n, d_in, d_out)
+    ws = _dense_ws(nbytes, dev)
     _check(lib.ezsp_linear(
         x.data_ptr(), ldx, n, d_in, d_out, TYPE_CODES[ty], w.data_ptr(),
         _at(bias), code, _at(residual), ldr, y.data_ptr(), d_out,
         TYPE_CODES[out_dtype], _at(z), d_out, ws.data_ptr(), nbytes,
-        _stream(dev)), "ezsp_linear")
+        _raw_stream(dev.index)), "ezsp_linear")
     return (y, z) if want_z else y
 
 
@@ -689,13 +709,13 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor,
     dw = torch.empty((d_in, d_out), dtype=ty, device=dev) if want_dw else None
     db = torch.empty(d_out, dtype=torch.float32, device=dev) \
         if want_db else None
-    nbytes = lib.ezsp_linear_backward_workspace_size(n, d_in, d_out,
-                                                     TYPE_CODES[ty])
-    ws = _workspace(nbytes, dev)
+    nbytes = _dense_bytes("ezsp_linear_backward_workspace_size", n, d_in,
+                          d_out, TYPE_CODES[ty])
+    ws = _dense_ws(nbytes, dev)
     _check(lib.ezsp_linear_backward(
         dy.data_ptr(), lddy, TYPE_CODES[dy.dtype], x.data_ptr(), ldx, n, d_in,
         d_out, TYPE_CODES[ty], w.data_ptr(), _at(z), ldz, code, _at(dx), d_in,
-        _at(dw), _at(db), ws.data_ptr(), nbytes, _stream(dev)),
+        _at(dw), _at(db), ws.data_ptr(), nbytes, _raw_stream(dev.index)),
         "ezsp_linear_backward")
     return dx, dw, db
 
@@ -722,12 +742,13 @@ def gated_ff(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor,
     gate = up = None
     if want_saved:
         gate, up = torch.empty_like(h), torch.empty_like(h)
-    nbytes = lib.ezsp_gated_ff_workspace_size(n, d_in, d_out)
-    ws = _workspace(nbytes, dev)
+    nbytes = _dense_bytes("ezsp_gated_ff_workspace_size", n, d_in, d_out)
+    ws = _dense_ws(nbytes, dev)
     _check(lib.ezsp_gated_ff(
         x.data_ptr(), ldx, n, d_in, d_out, TYPE_CODES[ty], w_gate.data_ptr(),
         _at(b_gate), w_up.data_ptr(), _at(b_up), code, h.data_ptr(), d_out,
-        _at(gate), _at(up), d_out, ws.data_ptr(), nbytes, _stream(dev)),
+        _at(gate), _at(up), d_out, ws.data_ptr(), nbytes,
+        _raw_stream(dev.index)),
         "ezsp_gated_ff")
     return (h, gate, up) if want_saved else h
 
@@ -760,13 +781,14 @@ def gated_ff_backward(dh: torch.Tensor, x: torch.Tensor,
     if want_db:
         dbg = torch.empty(d_out, dtype=torch.float32, device=dev)
         dbu = torch.empty(d_out, dtype=torch.float32, device=dev)
-    nbytes = lib.ezsp_gated_ff_backward_workspace_size(n, d_in, d_out,
-                                                       TYPE_CODES[ty])
-    ws = _workspace(nbytes, dev)
+    nbytes = _dense_bytes("ezsp_gated_ff_backward_workspace_size", n, d_in,
+                          d_out, TYPE_CODES[ty])
+    ws = _dense_ws(nbytes, dev)
     _check(lib.ezsp_gated_ff_backward(
         dh.data_ptr(), lddh, x.data_ptr(), ldx, n, d_in, d_out,
         TYPE_CODES[ty], w_gate.data_ptr(), w_up.data_ptr(), gate.data_ptr(),
         up.data_ptr(), lds, code, _at(dx), d_in, _at(dwg), _at(dwu),
-        _at(dbg), _at(dbu), ws.data_ptr(), nbytes, _stream(dev)),
+        _at(dbg), _at(dbu), ws.data_ptr(), nbytes,
+        _raw_stream(dev.index)),
         "ezsp_gated_ff_backward")
     return dx, dwg, dwu, dbg, dbu

@@ -22,6 +22,9 @@ SIZES = [
     (7, 12, 20), (8, 5, 3), (65, 31, 33), (700, 32, 40), (700, 20, 250),
     (700, 60, 30), (700, 64, 64), (700, 57, 200), (700, 100, 30),
     (700, 128, 64), (700, 97, 100), (20_000, 3, 7),
+    # few rows: columns and sums that fill no step, wide tables of weights
+    (1, 33, 9), (5, 70, 37), (48, 129, 333), (64, 8192, 16), (2, 4097, 70),
+    (1, 40, 16_400), (17, 40, 33_000), (40, 24, 40_001),
 ]
 EXACT = SIZES + [(4096, 64, 1600), (3333, 200, 2056), (70, 20_000, 40),
                  (20, 30_001, 9), (50_021, 16, 24)]

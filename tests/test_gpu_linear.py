@@ -23,6 +23,9 @@ SIZES = [
     (7, 12, 20), (8, 5, 3), (65, 31, 33), (700, 32, 128), (700, 20, 250),
     (700, 30, 400), (700, 60, 64), (700, 64, 500), (700, 100, 30),
     (700, 128, 100), (700, 97, 256), (20_000, 3, 7),
+    # few rows: columns and sums that fill no step, wide tables of weights
+    (1, 33, 9), (5, 70, 37), (48, 129, 333), (64, 8192, 16), (2, 4097, 70),
+    (1, 40, 16_400), (17, 40, 33_000), (40, 24, 40_001),
 ]
 
 
