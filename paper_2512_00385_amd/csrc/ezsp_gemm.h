@@ -94,6 +94,8 @@ typedef short s16x4_t __attribute__((ext_vector_type(4)));
 typedef short s16x8_t __attribute__((ext_vector_type(8)));
 
 constexpr int64_t kCus = 256;    // of an MI355X
+// row distances that keep a tile's offsets in 32 bits
+constexpr int64_t kFastLd = (int64_t)1 << 21;
 constexpr int kLineBytes = 128;  // bytes of k in an LDS tile
 
 // One operand's LDS tile: R rows (its own index) by 128 bytes of k.
@@ -114,8 +116,10 @@ struct Tile {
     return 0;
   }
 
-  uint32_t off[FAST ? kCh : 1];
+  uint32_t off[kCh];              // bytes from the tile's first element
   u32x4_t reg[FAST ? 1 : kCh];
+  int32_t first, edge;            // !FAST: first row; rows left if not R
+  bool slow, raw;                 // no vector fits a line; reg as loaded
 
   // where piece i of this thread comes from: (row, k) of its first element
   static __device__ __forceinline__ void place(int i, int &r, int &k) {
@@ -129,30 +133,35 @@ struct Tile {
     }
   }
 
-  // FAST: byte offsets from the tile's first element.  Rows past the end
+  // A tile of rows row0 .. row0 + R - 1 out of rows.  Rows past the end
   // repeat the last one: they only feed elements of D that do not exist.
-  __device__ __forceinline__ void init(int32_t rows_left, int64_t ld) {
-    if constexpr (FAST) {
+  // Without FAST a piece of a line that ends inside it is loaded as the
+  // line's last kPer values and shifted into place by put().
+  __device__ __forceinline__ void init(int32_t row0, int32_t rows,
+                                       int64_t ld) {
+    const int32_t left = rows - row0;
+    first = row0;
+    edge = left < R ? left : 0;
+    slow = !FAST && (ld >= kFastLd || (!KMAJOR && rows < kPer));
+    raw = false;
 #pragma unroll
-      for (int i = 0; i < kCh; ++i) {
-        int r, k;
-        place(i, r, k);
-        if constexpr (KMAJOR) {
-          r = min(r, rows_left - 1);
-          off[i] = (uint32_t)(((int64_t)r * ld + k) * (int)sizeof(T));
-        } else {
-          r = min(r, rows_left - kPer);
-          off[i] = (uint32_t)(((int64_t)k * ld + r) * (int)sizeof(T));
-        }
+    for (int i = 0; i < kCh; ++i) {
+      int r, k;
+      place(i, r, k);
+      if constexpr (KMAJOR) {
+        r = min(r, left - 1);
+        off[i] = (uint32_t)(((int64_t)r * ld + k) * (int)sizeof(T));
+      } else {
+        r = min(r, left - kPer) + (FAST ? 0 : row0);
+        off[i] = (uint32_t)(((int64_t)k * ld + r) * (int)sizeof(T));
       }
     }
   }
 
-  // Starts bringing in the tile whose first element is p; rows_left and
-  // k_left count what exists from there on.
-  __device__ __forceinline__ void fetch(const T *p, int64_t ld,
-                                        int32_t rows_left, int32_t k_left,
-                                        char *lds) {
+  // Starts bringing in the tile whose first element is p; k_left counts the
+  // k that exist from there on.
+  __device__ __forceinline__ void fetch(const T *p, int64_t ld, int32_t rows,
+                                        int32_t k_left, char *lds) {
     if constexpr (FAST) {
       const uint32_t dst = __builtin_amdgcn_readfirstlane(
           lds_addr(lds) + (threadIdx.x / kWave) * (kWave * 16));
@@ -171,7 +180,19 @@ struct Tile {
                         dst + i * NT * 16);
         }
       }
+    } else if (k_left >= kK && !slow) {
+      const char *src = static_cast<const char *>(
+          uniform(KMAJOR ? p : p - first));
+#pragma unroll
+      for (int i = 0; i < kCh; ++i) {
+        if constexpr (sizeof(T) == 2)
+          reg[i] = *reinterpret_cast<const u32x4_u2 *>(src + off[i]);
+        else
+          reg[i] = *reinterpret_cast<const u32x4_u4 *>(src + off[i]);
+      }
+      raw = true;
     } else {
+      const int32_t rows_left = rows - first;
 #pragma unroll
       for (int i = 0; i < kCh; ++i) {
         int r, k;
@@ -201,6 +222,7 @@ struct Tile {
         }
         reg[i] = v;
       }
+      raw = false;
     }
   }
 
@@ -208,10 +230,26 @@ struct Tile {
   __device__ __forceinline__ void put(char *lds) {
     if constexpr (!FAST) {
 #pragma unroll
-      for (int i = 0; i < kCh; ++i)
+      for (int i = 0; i < kCh; ++i) {
+        u32x4_t v = reg[i];
+        if (!KMAJOR && raw && edge) {
+          int r, k;
+          place(i, r, k);
+          const int by = r - min(r, edge - kPer);  // elements
+          if (by > 0) {
+            uint64_t lo = ((uint64_t)v[1] << 32) | v[0];
+            uint64_t hi = ((uint64_t)v[3] << 32) | v[2];
+            const int bits = min(by * (int)sizeof(T) * 8, 127);
+            lo = bits >= 64 ? hi >> (bits & 63)
+                            : (lo >> bits) | (hi << (64 - bits));
+            hi = bits >= 64 ? 0 : hi >> bits;
+            v = u32x4_t{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi,
+                        (uint32_t)(hi >> 32)};
+          }
+        }
         *reinterpret_cast<u32x4_t *>(lds +
-                                     (i * NT + (int)threadIdx.x) * 16) =
-            reg[i];
+                                     (i * NT + (int)threadIdx.x) * 16) = v;
+      }
     }
   }
 
@@ -288,6 +326,8 @@ struct Shape {
   // waves whose part fits one stage; the others' lie past both
   static constexpr int kFit = kStage / kOut < WM * WN ? kStage / kOut : WM * WN;
   static constexpr int kLds = 2 * kStage + (WM * WN - kFit) * kOut;
+  // waves a SIMD is to hold: those of the blocks that LDS lets in
+  static constexpr int kWaves = 160 * 1024 / kLds * WM * WN / 4;
 };
 
 // Logical tile of block b out of total: XCD x takes the x-th contiguous run
@@ -320,8 +360,8 @@ __device__ __forceinline__ void tile_of(int32_t b, int32_t total,
 //    the barrier between two steps has multiplications to hide behind.
 // During an epilogue the next tile's first step is on its way.
 template <class S, class Epi>
-__global__ __launch_bounds__(S::NT) void k_gemm(GemmArgs<typename S::T> g,
-                                                Epi epi) {
+__global__ __launch_bounds__(S::NT, S::kWaves) void k_gemm(
+    GemmArgs<typename S::T> g, Epi epi) {
   typedef typename S::T T;
   __shared__ __attribute__((aligned(16))) char stages[S::kLds];
   const int lane = threadIdx.x & (kWave - 1);
@@ -342,9 +382,9 @@ __global__ __launch_bounds__(S::NT) void k_gemm(GemmArgs<typename S::T> g,
     n0 = tn * S::CN;
     f_t = sp * g.kt_split;
     f_end = min(kt_all, f_t + g.kt_split);
-    ta.init(g.m - m0, g.lda);
+    ta.init(m0, g.m, g.lda);
 #pragma unroll
-    for (int p = 0; p < S::NB; ++p) tb[p].init(g.n - n0, g.ldb);
+    for (int p = 0; p < S::NB; ++p) tb[p].init(n0, g.n, g.ldb);
   };
   auto fetch = [&](char *st) {
     if (f_blk >= total) return;
@@ -353,13 +393,13 @@ __global__ __launch_bounds__(S::NT) void k_gemm(GemmArgs<typename S::T> g,
     const T *a = second ? g.a[1] : g.a[0];
     ta.fetch(S::AK ? a + (int64_t)m0 * g.lda + k0
                    : a + (int64_t)k0 * g.lda + m0,
-             g.lda, g.m - m0, g.k - k0, st);
+             g.lda, g.m, g.k - k0, st);
 #pragma unroll
     for (int p = 0; p < S::NB; ++p) {
       const T *b = (second || p) ? g.b[1] : g.b[0];
       tb[p].fetch(S::BK ? b + (int64_t)n0 * g.ldb + k0
                         : b + (int64_t)k0 * g.ldb + n0,
-                  g.ldb, g.n - n0, g.k - k0,
+                  g.ldb, g.n, g.k - k0,
                   st + S::TileA::kBytes + p * S::TileB::kBytes);
     }
     if (++f_t == f_end) {
@@ -489,40 +529,70 @@ __global__ __launch_bounds__(S::NT) void k_gemm(GemmArgs<typename S::T> g,
 }
 
 // The parts of a split sum, added in order, through the epilogue.  kJoinAhead
-// parts are loaded at once: one after the other, their latencies would cost
-// more than the product they end.
+// parts are loaded at once, and with SL > 1 a block's SL slices of 64 threads
+// take every SL-th part and meet in LDS: one load after the other, the
+// latencies would cost more than the product they end.
 constexpr int kJoinAhead = 8;
-template <int NB, class Epi>
-__global__ __launch_bounds__(64) void k_gemm_join(int32_t splits, int32_t m,
-                                                  int32_t n, Epi epi) {
+constexpr int kJoinSlices = 16;
+template <int NB, int SL, class Epi>
+__global__ __launch_bounds__(64 * SL) void k_gemm_join(int32_t splits,
+                                                       int32_t m, int32_t n,
+                                                       Epi epi) {
+  __shared__ f32x4_t meet[SL > 1 ? SL : 1][SL > 1 ? 2 * NB : 1][64];
   const int32_t per_row = (n + kVec - 1) / kVec;
   const int64_t items = (int64_t)m * per_row;
   const int64_t next = (int64_t)NB * m * n;  // from part to part
-  for (int64_t it = (int64_t)blockIdx.x * 64 + threadIdx.x; it < items;
-       it += (int64_t)gridDim.x * 64) {
+  const int lane = threadIdx.x % 64, slice = threadIdx.x / 64;
+  // (a block's threads take the same number of steps)
+  for (int64_t i0 = (int64_t)blockIdx.x * 64; i0 < items;
+       i0 += (int64_t)gridDim.x * 64) {
+    const int64_t it = i0 + lane;
     const int32_t row = (int32_t)(it / per_row);
     const int32_t col = (int32_t)(it % per_row) * kVec;
-    const int32_t cnt = n - col;
+    const int32_t cnt = it < items ? n - col : 0;
     f32x8_t v[NB];
 #pragma unroll
     for (int p = 0; p < NB; ++p) {
       const float *src = epi.part + ((int64_t)p * m + row) * n + col;
       f32x8_t sum = f32x8_t(0.0f);
-      int32_t s = 0;
+      int32_t s = slice;
       if (cnt >= kVec) {
-        for (; s + kJoinAhead <= splits; s += kJoinAhead) {
+        for (; s + (kJoinAhead - 1) * SL < splits; s += kJoinAhead * SL) {
           f32x8_t t[kJoinAhead];
 #pragma unroll
           for (int q = 0; q < kJoinAhead; ++q)
-            t[q] = *reinterpret_cast<const f32x8_u *>(src + (s + q) * next);
+            t[q] =
+                *reinterpret_cast<const f32x8_u *>(src + (s + q * SL) * next);
 #pragma unroll
           for (int q = 0; q < kJoinAhead; ++q) sum += t[q];
         }
       }
-      for (; s < splits; ++s) sum += load8(src + s * next, cnt);
+      for (; s < splits; s += SL) sum += load8(src + s * next, cnt);
       v[p] = sum;
     }
-    epi.apply(row, col, cnt, v);
+    if constexpr (SL > 1) {
+      __syncthreads();
+#pragma unroll
+      for (int p = 0; p < NB; ++p) {
+        meet[slice][2 * p][lane] =
+            __builtin_shufflevector(v[p], v[p], 0, 1, 2, 3);
+        meet[slice][2 * p + 1][lane] =
+            __builtin_shufflevector(v[p], v[p], 4, 5, 6, 7);
+      }
+      __syncthreads();
+      if (slice) continue;
+#pragma unroll
+      for (int p = 0; p < NB; ++p) {
+        f32x4_t lo = meet[0][2 * p][lane], hi = meet[0][2 * p + 1][lane];
+#pragma unroll
+        for (int t = 1; t < SL; ++t) {
+          lo += meet[t][2 * p][lane];
+          hi += meet[t][2 * p + 1][lane];
+        }
+        v[p] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      }
+    }
+    if (cnt > 0) epi.apply(row, col, cnt, v);
   }
 }
 
@@ -595,7 +665,7 @@ struct EpiStore : EpiParts<NB> {
 inline bool fast_operand(const void *p, int64_t ld, int32_t contiguous,
                          int32_t bytes) {
   return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld * bytes % 16 == 0 &&
-         contiguous * bytes % 16 == 0 && ld < ((int64_t)1 << 21);
+         contiguous * bytes % 16 == 0 && ld < kFastLd;
 }
 
 template <class S, class Epi>
@@ -622,10 +692,15 @@ void gemm_launch(GemmArgs<typename S::T> g, const Epi &epi, int32_t splits,
                      dim3(S::NT), 0, st, g, epi);
   if (g.splits > 1) {
     const int64_t items = (int64_t)g.m * ((g.n + kVec - 1) / kVec);
-    hipLaunchKernelGGL((k_gemm_join<S::NB, Epi>),
-                       dim3((unsigned)std::min<int64_t>((items + 63) / 64,
-                                                        1 << 18)),
-                       dim3(64), 0, st, g.splits, g.m, g.n, epi);
+    const dim3 grid(
+        (unsigned)std::min<int64_t>((items + 63) / 64, (int64_t)1 << 18));
+    if (g.splits >= 2 * kJoinSlices)
+      hipLaunchKernelGGL((k_gemm_join<S::NB, kJoinSlices, Epi>), grid,
+                         dim3(64 * kJoinSlices), 0, st, g.splits, g.m, g.n,
+                         epi);
+    else
+      hipLaunchKernelGGL((k_gemm_join<S::NB, 1, Epi>), grid, dim3(64), 0, st,
+                         g.splits, g.m, g.n, epi);
   }
 }
 
