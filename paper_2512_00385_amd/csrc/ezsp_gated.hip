@@ -34,8 +34,8 @@ struct PrepGated {
   __device__ __forceinline__ void put(int64_t row, int32_t col, int32_t cnt,
                                       const f32x8_t *v) const {
     if (!dz) return;
-    store8(dz + row * lddz + col, v[0], cnt);
-    store8(dz + row * lddz + half + col, v[1], cnt);
+    store8(dz + row * lddz + col, v[0], kVec);  // zeros past the end
+    store8(dz + row * lddz + half + col, v[1], kVec);
   }
 };
 
@@ -161,6 +161,7 @@ void backward(const GatedArgs &a, hipStream_t st) {
     g.m = a.n;
     g.n = a.d_in;
     g.k = a.d_out;
+    g.ka = (int32_t)half;
     EpiStore<T, 1> e;
     e.part = a.part;
     e.out[0] = static_cast<T *>(a.dx);
@@ -168,6 +169,7 @@ void backward(const GatedArgs &a, hipStream_t st) {
     gemm<T, true, true, kSeq>(g, e, a.part_bytes, st);
   }
   if (a.dw_gate || a.dw_up) {
+    g = GemmArgs<T>{};
     g.a[0] = g.a[1] = static_cast<const T *>(a.x);
     g.lda = a.ldx;
     g.b[0] = dz;
@@ -176,6 +178,7 @@ void backward(const GatedArgs &a, hipStream_t st) {
     g.m = a.d_in;
     g.n = a.d_out;
     g.k = a.n;
+    g.rb = (int32_t)half;
     EpiStore<T, 2> e;
     e.part = a.part;
     e.out[0] = static_cast<T *>(a.dw_gate);

@@ -41,9 +41,13 @@ struct GemmArgs {
   const T *b[2];
   int64_t lda, ldb;
   int32_t m, n, k;  // k of one (A, B) pair
+  // what is stored of each operand: its own index and k.  Beyond m, n and k
+  // where it is padded (a workspace matrix; k with zeros), else those (0).
+  int32_t ra, rb, ka, kb;
   int32_t tiles_m, tiles_n;
   int32_t splits;   // the sum over k in this many parts
   int32_t kt_split; // LDS tiles of k per part
+  bool to_parts;    // the parts go to the workspace
 };
 
 // Lines that read as zero, for pieces past the end of k.
@@ -382,9 +386,9 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void k_gemm(
     n0 = tn * S::CN;
     f_t = sp * g.kt_split;
     f_end = min(kt_all, f_t + g.kt_split);
-    ta.init(m0, g.m, g.lda);
+    ta.init(m0, g.ra, g.lda);
 #pragma unroll
-    for (int p = 0; p < S::NB; ++p) tb[p].init(n0, g.n, g.ldb);
+    for (int p = 0; p < S::NB; ++p) tb[p].init(n0, g.rb, g.ldb);
   };
   auto fetch = [&](char *st) {
     if (f_blk >= total) return;
@@ -393,13 +397,13 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void k_gemm(
     const T *a = second ? g.a[1] : g.a[0];
     ta.fetch(S::AK ? a + (int64_t)m0 * g.lda + k0
                    : a + (int64_t)k0 * g.lda + m0,
-             g.lda, g.m, g.k - k0, st);
+             g.lda, g.ra, g.ka - k0, st);
 #pragma unroll
     for (int p = 0; p < S::NB; ++p) {
       const T *b = (second || p) ? g.b[1] : g.b[0];
       tb[p].fetch(S::BK ? b + (int64_t)n0 * g.ldb + k0
                         : b + (int64_t)k0 * g.ldb + n0,
-                  g.ldb, g.n, g.k - k0,
+                  g.ldb, g.rb, g.kb - k0,
                   st + S::TileA::kBytes + p * S::TileB::kBytes);
     }
     if (++f_t == f_end) {
@@ -514,7 +518,7 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void k_gemm(
           v[p] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         }
         if (row < g.m && col < g.n) {
-          if (g.splits == 1)
+          if (!g.to_parts)
             epi.apply(row, col, g.n - col, v);
           else
             epi.partial(tile_sp, g.m, g.n, row, col, v);
@@ -620,6 +624,14 @@ struct EpiLinear : EpiParts<1> {
   void *z;
   int64_t ldz;
   int32_t type, type_y, act;
+  void shift(int64_t rows) {  // rows of D further on
+    auto on = [&](const void *p, int64_t ld, int t) {
+      return p ? (char *)p + rows * ld * (int64_t)type_bytes(t) : nullptr;
+    };
+    res = on(res, ldr, type_y);
+    y = on(y, ldy, type_y);
+    z = on(z, ldz, type);
+  }
   __device__ __forceinline__ void apply(int32_t row, int32_t col, int32_t cnt,
                                         f32x8_t *v) const {
     if (bias) v[0] += load8(bias + col, cnt);
@@ -637,6 +649,11 @@ struct EpiGated : EpiParts<2> {
   T *h, *gate, *up;
   int64_t ldh, lds;
   int32_t act;
+  void shift(int64_t rows) {
+    h += rows * ldh;
+    if (gate) gate += rows * lds;
+    if (up) up += rows * lds;
+  }
   __device__ __forceinline__ void apply(int32_t row, int32_t col, int32_t cnt,
                                         f32x8_t *v) const {
 #pragma unroll
@@ -653,6 +670,10 @@ template <class T, int NB>
 struct EpiStore : EpiParts<NB> {
   T *out[NB];
   int64_t ld;
+  void shift(int64_t rows) {
+    for (T *&o : out)
+      if (o) o += rows * ld;
+  }
   __device__ __forceinline__ void apply(int32_t row, int32_t col, int32_t cnt,
                                         f32x8_t *v) const {
 #pragma unroll
@@ -669,14 +690,30 @@ inline bool fast_operand(const void *p, int64_t ld, int32_t contiguous,
 }
 
 template <class S, class Epi>
-void gemm_launch(GemmArgs<typename S::T> g, const Epi &epi, int32_t splits,
-                 hipStream_t st) {
+void gemm_join(int32_t splits, int32_t m, int32_t n, const Epi &epi,
+               hipStream_t st) {
+  const int64_t items = (int64_t)m * ((n + kVec - 1) / kVec);
+  const dim3 grid(
+      (unsigned)std::min<int64_t>((items + 63) / 64, (int64_t)1 << 18));
+  if (splits >= 2 * kJoinSlices)
+    hipLaunchKernelGGL((k_gemm_join<S::NB, kJoinSlices, Epi>), grid,
+                       dim3(64 * kJoinSlices), 0, st, splits, m, n, epi);
+  else
+    hipLaunchKernelGGL((k_gemm_join<S::NB, 1, Epi>), grid, dim3(64), 0, st,
+                       splits, m, n, epi);
+}
+
+// parts_only: the sum's parts stay in epi.part, however many (a longer sum's
+// share); returns their number.
+template <class S, class Epi>
+int32_t gemm_launch(GemmArgs<typename S::T> g, const Epi &epi, int32_t splits,
+                    bool parts_only, hipStream_t st) {
   g.tiles_m = (g.m + S::BM - 1) / S::BM;
   g.tiles_n = (g.n + S::CN - 1) / S::CN;
   const int32_t kt = (g.k + S::kK - 1) / S::kK * (S::MODE == kSeq ? 2 : 1);
-  g.splits = splits;
   g.kt_split = (kt + splits - 1) / splits;
   g.splits = (kt + g.kt_split - 1) / g.kt_split;  // no empty part
+  g.to_parts = parts_only || g.splits > 1;
   const int64_t total = (int64_t)g.tiles_m * g.tiles_n * g.splits;
   // as many blocks as the chip holds at once
   static const int64_t slots = [] {
@@ -690,23 +727,15 @@ void gemm_launch(GemmArgs<typename S::T> g, const Epi &epi, int32_t splits,
   hipLaunchKernelGGL((k_gemm<S, Epi>),
                      dim3((unsigned)std::min<int64_t>(total, slots)),
                      dim3(S::NT), 0, st, g, epi);
-  if (g.splits > 1) {
-    const int64_t items = (int64_t)g.m * ((g.n + kVec - 1) / kVec);
-    const dim3 grid(
-        (unsigned)std::min<int64_t>((items + 63) / 64, (int64_t)1 << 18));
-    if (g.splits >= 2 * kJoinSlices)
-      hipLaunchKernelGGL((k_gemm_join<S::NB, kJoinSlices, Epi>), grid,
-                         dim3(64 * kJoinSlices), 0, st, g.splits, g.m, g.n,
-                         epi);
-    else
-      hipLaunchKernelGGL((k_gemm_join<S::NB, 1, Epi>), grid, dim3(64), 0, st,
-                         g.splits, g.m, g.n, epi);
-  }
+  if (g.splits > 1 && !parts_only)
+    gemm_join<S>(g.splits, g.m, g.n, epi, st);
+  return g.splits;
 }
 
 // Splits of a sum over k for a product of `tiles` tiles: enough blocks for
-// two a CU, four LDS tiles a part at least, and no more parts than the
-// workspace holds.
+// two a CU, eight steps a part at least (a join costs what ten steps of a
+// lone block do; four where 32 rows make a step short: one token, 4096 ->
+// 4096, takes 12.0 us in 16 parts and 13.5 in 8), and no more parts than fit.
 template <class S>
 int32_t gemm_splits(const GemmArgs<typename S::T> &g, size_t part_bytes) {
   const int64_t tiles = (int64_t)((g.m + S::BM - 1) / S::BM) *
@@ -714,20 +743,19 @@ int32_t gemm_splits(const GemmArgs<typename S::T> &g, size_t part_bytes) {
   const int64_t kt = ((int64_t)g.k + S::kK - 1) / S::kK *
                      (S::MODE == kSeq ? 2 : 1);
   const int64_t one = (int64_t)g.m * g.n * S::NB * 4;
-  int64_t s = std::min<int64_t>(512 / std::max<int64_t>(tiles, 1), kt / 4);
+  int64_t s = std::min<int64_t>(512 / std::max<int64_t>(tiles, 1),
+                                kt / (S::BM == 32 ? 4 : 8));
   s = std::min<int64_t>(s, (int64_t)(part_bytes / (size_t)one));
   return (int32_t)std::max<int64_t>(s, 1);
 }
 
-// Tile of the block by the shape of D.
-template <class T, bool AK, bool BK, int MODE, bool FAST, class Epi>
-void gemm_shape(const GemmArgs<T> &g, const Epi &epi, size_t part_bytes,
-                hipStream_t st) {
-#define EZSP_GEMM(BM, BN, WM, WN)                                          \
-  do {                                                                     \
-    typedef Shape<T, BM, BN, WM, WN, AK, BK, MODE, FAST> S;                \
-    gemm_launch<S>(g, epi, gemm_splits<S>(g, part_bytes), st);             \
-    return;                                                                \
+// Tile of the block by the shape of D; f gets its Shape.
+template <class T, bool AK, bool BK, int MODE, bool FAST, class F>
+void gemm_shape(const GemmArgs<T> &g, F f) {
+#define EZSP_GEMM(BM, BN, WM, WN)                            \
+  do {                                                       \
+    f(Shape<T, BM, BN, WM, WN, AK, BK, MODE, FAST>{});       \
+    return;                                                  \
   } while (0)
   constexpr int kB = MODE == kDual ? 2 : 1;
   if (g.m <= 32) EZSP_GEMM(32, 128, 1, kB == 2 ? 2 : 4);
@@ -742,20 +770,142 @@ void gemm_shape(const GemmArgs<T> &g, const Epi &epi, size_t part_bytes,
 #undef EZSP_GEMM
 }
 
-// D = A B through epi; part_bytes is what epi.part holds.
+// --- packing ----------------------------------------------------------------
+// Rows [rows][cols] at any alignment into rows of ldp (a multiple of kVec)
+// values, zero past cols.
+template <class T>
+__global__ __launch_bounds__(256) void k_pack(const T *__restrict__ src,
+                                              int64_t ld, int32_t rows,
+                                              int32_t cols,
+                                              T *__restrict__ dst,
+                                              int64_t ldp) {
+  const int32_t per_row = (int32_t)(ldp / kVec);
+  const int64_t items = (int64_t)rows * per_row;
+  for (int64_t it = (int64_t)blockIdx.x * 256 + threadIdx.x; it < items;
+       it += (int64_t)gridDim.x * 256) {
+    const int32_t row = (int32_t)(it / per_row);
+    const int32_t col = (int32_t)(it % per_row) * kVec;
+    store8(dst + row * ldp + col, load8(src + row * ld + col, cols - col),
+           kVec);
+  }
+}
+
+template <class T>
+void pack_launch(const T *src, int64_t ld, int32_t rows, int32_t cols, T *dst,
+                 hipStream_t st) {
+  const int64_t ldp = pad_row(cols);
+  const int64_t items = (int64_t)rows * (ldp / kVec);
+  hipLaunchKernelGGL(k_pack<T>,
+                     dim3((unsigned)std::min<int64_t>((items + 255) / 256,
+                                                      1 << 14)),
+                     dim3(256), 0, st, src, ld, rows, cols, dst, ldp);
+}
+
+// D = A B through epi, whose parts lie in the part_bytes at epi.part.
+//
+// Operands at 16-byte alignment go past the registers into LDS, others
+// through them, at a third of the rate in products that fill the chip.  There
+// an unaligned operand is first packed into the same workspace, W whole and
+// the long one in chunks of rows; a copy of it costs 2 k e bytes a row, which
+// 2 n k multiplications at the higher rate repay from n = kPackN on.
+constexpr double kPackFlops = 4e9;
+constexpr int32_t kPackN = 192;
+
 template <class T, bool AK, bool BK, int MODE, class Epi>
-void gemm(const GemmArgs<T> &g, const Epi &epi, size_t part_bytes,
-          hipStream_t st) {
-  const int32_t e = (int32_t)sizeof(T);
-  bool fast = fast_operand(g.a[0], g.lda, AK ? g.k : g.m, e) &&
-              fast_operand(g.b[0], g.ldb, BK ? g.k : g.n, e);
-  if (MODE == kSeq) fast = fast && fast_operand(g.a[1], g.lda, AK ? g.k : g.m, e);
+void gemm(GemmArgs<T> g, Epi epi, size_t part_bytes, hipStream_t st) {
+  constexpr int32_t e = (int32_t)sizeof(T);
+  constexpr int kB = MODE == kPlain ? 1 : 2;  // B matrices
+  if (!g.ra) g.ra = g.m;
+  if (!g.rb) g.rb = g.n;
+  if (!g.ka) g.ka = g.k;
+  if (!g.kb) g.kb = g.k;
+  bool fast_a = fast_operand(g.a[0], g.lda, AK ? g.ka : g.ra, e);
+  bool fast_b = fast_operand(g.b[0], g.ldb, BK ? g.kb : g.rb, e);
+  if (MODE == kSeq)
+    fast_a = fast_a && fast_operand(g.a[1], g.lda, AK ? g.ka : g.ra, e);
   if (MODE != kPlain)
-    fast = fast && fast_operand(g.b[1], g.ldb, BK ? g.k : g.n, e);
-  if (fast)
-    gemm_shape<T, AK, BK, MODE, true>(g, epi, part_bytes, st);
+    fast_b = fast_b && fast_operand(g.b[1], g.ldb, BK ? g.kb : g.rb, e);
+
+  char *space = reinterpret_cast<char *>(epi.part);
+  size_t room = part_bytes & ~(size_t)255;
+  const double flops = 2.0 * g.m * g.n * (double)g.k * kB;
+  if ((!fast_a || !fast_b) && flops >= kPackFlops &&
+      (fast_a || (MODE != kSeq && (AK ? g.n : g.n + 64) * kB >= kPackN))) {
+    const int64_t b_rows = BK ? g.n : g.k, b_cols = BK ? g.k : g.n;
+    const size_t b_bytes =
+        fast_b ? 0 : (size_t)(b_rows * pad_row(b_cols)) * e * kB;
+    if (b_bytes <= room / 2) {
+      if (!fast_b) {
+        room = (room - b_bytes) & ~(size_t)255;
+        T *dst = reinterpret_cast<T *>(space + room);
+        for (int p = 0; p < kB; ++p) {
+          pack_launch(g.b[p], g.ldb, (int32_t)b_rows, (int32_t)b_cols,
+                      dst + p * b_rows * pad_row(b_cols), st);
+          g.b[p] = dst + p * b_rows * pad_row(b_cols);
+        }
+        g.ldb = pad_row(b_cols);
+        (BK ? g.kb : g.rb) = (int32_t)g.ldb;
+        fast_b = true;
+      }
+      // rows of A at a time that fit half of the room
+      const int64_t a_rows = AK ? g.m : g.k, a_cols = AK ? g.k : g.m;
+      const int64_t a_row = pad_row(a_cols) * e;
+      const int64_t fit = (int64_t)(room / 2) / a_row / 256 * 256;
+      if (!fast_a && (fit >= a_rows || fit >= 8192)) {
+        const int64_t chunk = std::min(fit, a_rows);
+        room = (room - (size_t)(chunk * a_row)) & ~(size_t)255;
+        T *dst = reinterpret_cast<T *>(space + room);
+        const T *src = g.a[0];
+        const int64_t ld = g.lda;
+        GemmArgs<T> c = g;
+        c.a[0] = c.a[1] = dst;
+        c.lda = pad_row(a_cols);
+        (AK ? c.ka : c.ra) = (int32_t)c.lda;
+        if (AK) {
+          for (int64_t r = 0; r < a_rows; r += chunk) {
+            c.m = c.ra = (int32_t)std::min(chunk, a_rows - r);
+            pack_launch(src + r * ld, ld, c.m, (int32_t)a_cols, dst, st);
+            gemm_shape<T, AK, BK, MODE, true>(c, [&](auto s) {
+              typedef decltype(s) S;
+              gemm_launch<S>(c, epi, gemm_splits<S>(c, room), false, st);
+            });
+            epi.shift(c.m);
+          }
+          return;
+        }
+        // chunks of the sum: their parts side by side, joined at the end
+        gemm_shape<T, AK, BK, MODE, true>(c, [&](auto s) {
+          typedef decltype(s) S;
+          const int64_t chunks = (a_rows + chunk - 1) / chunk;
+          const size_t one = (size_t)g.m * g.n * S::NB * 4;
+          const int64_t all =
+              std::max<int64_t>(gemm_splits<S>(g, room), chunks);
+          const int64_t each = std::max<int64_t>(all / chunks, 1);
+          if (room / one < (size_t)(each * chunks)) return;  // as they lie
+          Epi at = epi;
+          int32_t parts = 0;
+          for (int64_t r = 0; r < a_rows; r += chunk) {
+            c.k = c.ka = c.kb = (int32_t)std::min(chunk, a_rows - r);
+            pack_launch(src + r * ld, ld, c.k, (int32_t)a_cols, dst, st);
+            for (int p = 0; p < kB; ++p) c.b[p] = g.b[p] + r * g.ldb;
+            at.part = epi.part + parts * (one / 4);
+            parts += gemm_launch<S>(c, at, (int32_t)each, true, st);
+          }
+          gemm_join<S>(parts, g.m, g.n, epi, st);
+          fast_a = true;
+        });
+        if (fast_a) return;
+      }
+    }
+  }
+  auto whole = [&](auto s) {
+    typedef decltype(s) S;
+    gemm_launch<S>(g, epi, gemm_splits<S>(g, room), false, st);
+  };
+  if (fast_a && fast_b)
+    gemm_shape<T, AK, BK, MODE, true>(g, whole);
   else
-    gemm_shape<T, AK, BK, MODE, false>(g, epi, part_bytes, st);
+    gemm_shape<T, AK, BK, MODE, false>(g, whole);
 }
 
 // --- gradients before their products ---------------------------------------

@@ -30,7 +30,7 @@ struct PrepLinear {
   }
   __device__ __forceinline__ void put(int64_t row, int32_t col, int32_t cnt,
                                       const f32x8_t *v) const {
-    if (dz) store8(dz + row * lddz + col, v[0], cnt);
+    if (dz) store8(dz + row * lddz + col, v[0], kVec);  // zeros past the end
   }
 };
 
@@ -92,9 +92,11 @@ void backward_narrow(const LinearArgs &a, hipStream_t st) {
                                    nullptr, a.db, nullptr, st);
 }
 
-// dz has to be formed unless dy is it already
+// dz has to be formed unless dy is it already, at an alignment that the
+// products take at their full rate
 bool needs_dz(const LinearArgs &a) {
-  return a.act != EZSP_ACT_NONE || a.type_y != a.type;
+  return a.act != EZSP_ACT_NONE || a.type_y != a.type ||
+         !fast_operand(a.dy, a.lddy, a.d_out, (int32_t)type_bytes(a.type));
 }
 
 template <class T>
@@ -169,11 +171,13 @@ void backward(const LinearArgs &a, hipStream_t st) {
     g.m = a.n;
     g.n = a.d_in;
     g.k = a.d_out;
+    if (form) g.ka = (int32_t)lddz;
     e.out[0] = static_cast<T *>(a.dx);
     e.ld = a.lddx;
     gemm<T, true, true, kPlain>(g, e, a.part_bytes, st);
   }
   if (a.dw) {
+    g = GemmArgs<T>{};
     g.a[0] = static_cast<const T *>(a.x);
     g.lda = a.ldx;
     g.b[0] = dz;
@@ -181,6 +185,7 @@ void backward(const LinearArgs &a, hipStream_t st) {
     g.m = a.d_in;
     g.n = a.d_out;
     g.k = a.n;
+    if (form) g.rb = (int32_t)lddz;
     e.out[0] = static_cast<T *>(a.dw);
     e.ld = a.d_out;
     gemm<T, false, false, kPlain>(g, e, a.part_bytes, st);

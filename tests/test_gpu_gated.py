@@ -27,7 +27,9 @@ SIZES = [
     (1, 40, 16_400), (17, 40, 33_000), (40, 24, 40_001),
 ]
 EXACT = SIZES + [(4096, 64, 1600), (3333, 200, 2056), (70, 20_000, 40),
-                 (20, 30_001, 9), (50_021, 16, 24)]
+                 (20, 30_001, 9), (50_021, 16, 24),
+                 # large and unaligned: packed, whole and in chunks
+                 (5001, 1021, 515), (190_001, 259, 264), (30_003, 67, 1030)]
 
 
 @pytest.fixture(scope="module", autouse=True)

@@ -89,7 +89,9 @@ def test_forward_activations(act, ty):
 # sums exact in fp32 whatever their order: results are the exact ones,
 # rounded; sizes that reach the largest tiles and split sums too
 EXACT = SIZES + [(4096, 64, 3200), (3333, 200, 4112), (70, 20_000, 40),
-                 (1, 65_536, 24), (20, 30_001, 9), (50_021, 16, 24)]
+                 (1, 65_536, 24), (20, 30_001, 9), (50_021, 16, 24),
+                 # large and unaligned: packed, whole and in chunks
+                 (5001, 1021, 515), (190_001, 259, 264), (30_003, 67, 1030)]
 
 
 @pytest.mark.parametrize("ty", [BF, F32])
