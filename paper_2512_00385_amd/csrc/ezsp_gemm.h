@@ -732,10 +732,11 @@ int32_t gemm_launch(GemmArgs<typename S::T> g, const Epi &epi, int32_t splits,
   return g.splits;
 }
 
-// Splits of a sum over k for a product of `tiles` tiles: enough blocks for
-// two a CU, eight steps a part at least (a join costs what ten steps of a
-// lone block do; four where 32 rows make a step short: one token, 4096 ->
-// 4096, takes 12.0 us in 16 parts and 13.5 in 8), and no more parts than fit.
+// Splits of a sum over k for a product of `tiles` tiles: enough blocks to
+// fill the chip (two a CU, or one of the largest), eight steps a part at least
+// (a join costs what ten steps of a lone block do; four where 32 rows make a
+// step short: one token, 4096 -> 4096, takes 12.0 us in 16 parts and 13.5 in
+// 8), and no more parts than fit.
 template <class S>
 int32_t gemm_splits(const GemmArgs<typename S::T> &g, size_t part_bytes) {
   const int64_t tiles = (int64_t)((g.m + S::BM - 1) / S::BM) *
@@ -743,31 +744,64 @@ int32_t gemm_splits(const GemmArgs<typename S::T> &g, size_t part_bytes) {
   const int64_t kt = ((int64_t)g.k + S::kK - 1) / S::kK *
                      (S::MODE == kSeq ? 2 : 1);
   const int64_t one = (int64_t)g.m * g.n * S::NB * 4;
-  int64_t s = std::min<int64_t>(512 / std::max<int64_t>(tiles, 1),
+  const int64_t blocks = S::BM * S::BN >= 256 * 256 ? kCus : 2 * kCus;
+  int64_t s = std::min<int64_t>(blocks / std::max<int64_t>(tiles, 1),
                                 kt / (S::BM == 32 ? 4 : 8));
   s = std::min<int64_t>(s, (int64_t)(part_bytes / (size_t)one));
   return (int32_t)std::max<int64_t>(s, 1);
 }
 
+// Time a step of a product in tiles of S, split as gemm_splits does: rounds
+// of per_cu blocks a CU at `full`, the last one at `one` where a block a CU is
+// enough for it.
+template <class S>
+double gemm_rounds(const GemmArgs<typename S::T> &g, size_t part_bytes,
+                   int per_cu, double one, double full) {
+  const int64_t splits = gemm_splits<S>(g, part_bytes);
+  const int64_t work = (int64_t)((g.m + S::BM - 1) / S::BM) *
+                       ((g.n + S::CN - 1) / S::CN) * splits;
+  const int64_t slots = per_cu * kCus;
+  const int64_t rest = work % slots;
+  return ((double)(work / slots) * full +
+          (rest == 0 ? 0.0 : rest <= kCus ? one : full)) /
+         (double)splits;
+}
+
 // Tile of the block by the shape of D; f gets its Shape.
 template <class T, bool AK, bool BK, int MODE, bool FAST, class F>
-void gemm_shape(const GemmArgs<T> &g, F f) {
-#define EZSP_GEMM(BM, BN, WM, WN)                            \
-  do {                                                       \
-    f(Shape<T, BM, BN, WM, WN, AK, BK, MODE, FAST>{});       \
-    return;                                                  \
+void gemm_shape(const GemmArgs<T> &g, size_t part_bytes, F f) {
+#define EZSP_SHAPE(BM, BN, WM, WN) \
+  Shape<T, BM, BN, WM, WN, AK, BK, MODE, FAST>
+#define EZSP_GEMM(BM, BN, WM, WN)      \
+  do {                                 \
+    f(EZSP_SHAPE(BM, BN, WM, WN){});   \
+    return;                            \
   } while (0)
   constexpr int kB = MODE == kDual ? 2 : 1;
   if (g.m <= 32) EZSP_GEMM(32, 128, 1, kB == 2 ? 2 : 4);
   if (g.n <= 32) EZSP_GEMM(128, 32 * kB, 4, 1);
+  // fp32 is bound by its matrix instructions at any tile, so the tile is the
+  // one that wastes the fewest (20,011 x 515: 785 tiles of 128 x 128 in two
+  // rounds of 512, at 53 %; 1413 of 128 x 64 at 82 %)
+  if constexpr (sizeof(T) == 4) {
+    if constexpr (MODE == kDual)
+      EZSP_GEMM(128, 64, 4, 1);
+    else
+      EZSP_GEMM(128, 64, 2, 2);
+  }
   if (g.n * kB <= 64) EZSP_GEMM(128, 64, 4, 1);
+  // microseconds a step: 1.47 for one 256 x 256 block a CU; 0.94 for two of
+  // 128 x 128, which hide each other's epilogues, 0.6 for one
   if constexpr (FAST && sizeof(T) == 2) {
-    const int64_t big = (int64_t)((g.m + 255) / 256) *
-                        ((g.n * kB + 255) / 256);
-    if (big >= 192) EZSP_GEMM(256, 256, 2, 4);
+    typedef EZSP_SHAPE(256, 256, 2, 4) L;
+    typedef EZSP_SHAPE(128, 128, 2, 2) M;
+    if (gemm_rounds<L>(g, part_bytes, 1, 1.47, 1.47) <
+        gemm_rounds<M>(g, part_bytes, 2, 0.6, 0.94))
+      EZSP_GEMM(256, 256, 2, 4);
   }
   EZSP_GEMM(128, 128, 2, 2);
 #undef EZSP_GEMM
+#undef EZSP_SHAPE
 }
 
 // --- packing ----------------------------------------------------------------
@@ -865,7 +899,7 @@ void gemm(GemmArgs<T> g, Epi epi, size_t part_bytes, hipStream_t st) {
           for (int64_t r = 0; r < a_rows; r += chunk) {
             c.m = c.ra = (int32_t)std::min(chunk, a_rows - r);
             pack_launch(src + r * ld, ld, c.m, (int32_t)a_cols, dst, st);
-            gemm_shape<T, AK, BK, MODE, true>(c, [&](auto s) {
+            gemm_shape<T, AK, BK, MODE, true>(c, room, [&](auto s) {
               typedef decltype(s) S;
               gemm_launch<S>(c, epi, gemm_splits<S>(c, room), false, st);
             });
@@ -874,7 +908,7 @@ void gemm(GemmArgs<T> g, Epi epi, size_t part_bytes, hipStream_t st) {
           return;
         }
         // chunks of the sum: their parts side by side, joined at the end
-        gemm_shape<T, AK, BK, MODE, true>(c, [&](auto s) {
+        gemm_shape<T, AK, BK, MODE, true>(c, room, [&](auto s) {
           typedef decltype(s) S;
           const int64_t chunks = (a_rows + chunk - 1) / chunk;
           const size_t one = (size_t)g.m * g.n * S::NB * 4;
@@ -903,9 +937,9 @@ void gemm(GemmArgs<T> g, Epi epi, size_t part_bytes, hipStream_t st) {
     gemm_launch<S>(g, epi, gemm_splits<S>(g, room), false, st);
   };
   if (fast_a && fast_b)
-    gemm_shape<T, AK, BK, MODE, true>(g, whole);
+    gemm_shape<T, AK, BK, MODE, true>(g, room, whole);
   else
-    gemm_shape<T, AK, BK, MODE, false>(g, whole);
+    gemm_shape<T, AK, BK, MODE, false>(g, room, whole);
 }
 
 // --- gradients before their products ---------------------------------------
