@@ -77,6 +77,93 @@ __device__ __forceinline__ void store8(float *p, f32x8_t v, int cnt) {
   }
 }
 
+// A lane's kVec columns from col on, of rows of d values.  They are loaded
+// without a branch, as they lie in memory: columns of an incomplete last
+// vector by way of the vector that ends with the row, rows past the end as
+// the last one.  settle() then shifts them into place and zeroes what does
+// not exist.  Rows shorter than a vector are loaded together with what
+// follows them, the table's last ones with what precedes them.
+struct Span {
+  int32_t at;   // column that the load starts at
+  int32_t cnt;  // columns that exist
+  int32_t off;  // first of them in the load
+  bool thin;    // d < kVec
+};
+__device__ __forceinline__ Span span_of(int32_t col, int32_t d) {
+  Span s;
+  s.cnt = min(max(d - col, 0), kVec);
+  s.at = min(col, max(d - kVec, 0));
+  s.off = col - s.at;
+  s.thin = d < kVec;
+  return s;
+}
+// rows [n] of the table and their distance; n * d >= kVec
+__device__ __forceinline__ int64_t span_at(int64_t row, int64_t ld, int32_t n,
+                                           int32_t d, Span s, int32_t &back) {
+  const int64_t at = min(row, (int64_t)n - 1) * ld + s.at;
+  back = 0;
+  if (s.thin) {
+    const int64_t last = (int64_t)(n - 1) * ld + d - kVec;
+    if (at > last) back = (int32_t)(at - last);
+  }
+  return at - back;
+}
+template <class T>
+struct Vec8;  // kVec values in registers
+template <>
+struct Vec8<__bf16> {
+  u32x4_t v;
+};
+template <>
+struct Vec8<float> {
+  f32x8_t v;
+};
+__device__ __forceinline__ Vec8<__bf16> raw8(const __bf16 *p) {
+  return {*reinterpret_cast<const u32x4_u2 *>(p)};
+}
+__device__ __forceinline__ Vec8<float> raw8(const float *p) {
+  return {*reinterpret_cast<const f32x8_u *>(p)};
+}
+// The same from load8, for tables of less than a vector.
+__device__ __forceinline__ Vec8<__bf16> raw_of(f32x8_t v, const __bf16 *) {
+  return {__builtin_bit_cast(u32x4_t, __builtin_convertvector(v, bf16x8_t))};
+}
+__device__ __forceinline__ Vec8<float> raw_of(f32x8_t v, const float *) {
+  return {v};
+}
+__device__ __forceinline__ bf16x8_t settle(Vec8<__bf16> r, int32_t off,
+                                           int32_t cnt) {
+  if (off) {
+    uint64_t lo = ((uint64_t)r.v[1] << 32) | r.v[0];
+    uint64_t hi = ((uint64_t)r.v[3] << 32) | r.v[2];
+    const int bits = 16 * off;  // those of 8 and more are zeroed below
+    lo = bits >= 64 ? hi >> (bits & 63)
+                    : (lo >> bits) | (hi << ((64 - bits) & 63));
+    hi = bits >= 64 ? 0 : hi >> bits;
+    r.v = u32x4_t{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi,
+                  (uint32_t)(hi >> 32)};
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    r.v[i] = cnt > 2 * i + 1 ? r.v[i] : cnt > 2 * i ? r.v[i] & 0xffffu : 0u;
+  return __builtin_bit_cast(bf16x8_t, r.v);
+}
+__device__ __forceinline__ f32x8_t settle(Vec8<float> r, int32_t off,
+                                          int32_t cnt) {
+  if (off) {
+#pragma unroll
+    for (int step = 4; step > 0; step >>= 1)
+      if (off & step) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i)
+          r.v[i] = i + step < kVec ? r.v[i + step] : 0.0f;
+      }
+  }
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) r.v[i] = i < cnt ? r.v[i] : 0.0f;
+  return r.v;
+}
+
 // Accesses whose element type is known at run time only (uniform branches).
 __device__ __forceinline__ f32x8_t load8_t(const void *p, int64_t at, int type,
                                            int cnt) {

@@ -51,8 +51,8 @@ struct NarrowGated {
                                      Span s) const {
     Raw r;
     int32_t back;
-    r.d = raw8(dh + span_at<__bf16>(row, lddh, n, d, s, back));
-    const int64_t at = span_at<__bf16>(row, lds, n, d, s, back);
+    r.d = raw8(dh + span_at(row, lddh, n, d, s, back));
+    const int64_t at = span_at(row, lds, n, d, s, back);
     r.g = raw8(gate + at);
     r.u = raw8(up + at);
     return r;
@@ -61,12 +61,12 @@ struct NarrowGated {
                                         int32_t d, Span s, f32x8_t *v) const {
     const int32_t cnt = row < n ? s.cnt : 0;
     int32_t back;
-    span_at<__bf16>(row, lds, n, d, s, back);
+    span_at(row, lds, n, d, s, back);
     const f32x8_t g =
         __builtin_convertvector(settle(r.g, s.off + back, cnt), f32x8_t);
     const f32x8_t u =
         __builtin_convertvector(settle(r.u, s.off + back, cnt), f32x8_t);
-    span_at<__bf16>(row, lddh, n, d, s, back);
+    span_at(row, lddh, n, d, s, back);
     const f32x8_t dv =
         __builtin_convertvector(settle(r.d, s.off + back, cnt), f32x8_t);
     f32x8_t a, da;
@@ -95,9 +95,11 @@ void backward_narrow(const GatedArgs &a, hipStream_t st) {
   op.lddh = a.lddh;
   op.lds = a.lds;
   op.act = a.act;
-  narrow<NarrowGated, 2>(g, op, static_cast<__bf16 *>(a.dw_gate),
-                         static_cast<__bf16 *>(a.dw_up), a.db_gate, a.db_up,
-                         st);
+  g.dw[0] = static_cast<__bf16 *>(a.dw_gate);
+  g.dw[1] = static_cast<__bf16 *>(a.dw_up);
+  g.db[0] = a.db_gate;
+  g.db[1] = a.db_up;
+  narrow<NarrowGated, 2>(g, op, st);
 }
 
 template <class T>

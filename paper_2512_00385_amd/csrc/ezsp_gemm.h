@@ -946,7 +946,9 @@ void gemm(GemmArgs<T> g, Epi epi, size_t part_bytes, hipStream_t st) {
 // Op::at gives the gradients of NB pre-activations at kVec neighbouring
 // columns of a row, Op::put stores them; the column sums (the biases'
 // gradients) are kept in registers over a block's rows, in fp32 and before
-// any rounding, and joined over the block: part[block row][NB * m].
+// any rounding, and joined over the block: part[p] is product p's row of m,
+// stride from block row to block row, or the result itself where one block
+// row takes all rows.
 constexpr int kPrepNT = 256;
 constexpr int kPrepCols = 16;                    // column groups of a block
 constexpr int kPrepRows = kPrepNT / kPrepCols;   // rows of a step
@@ -954,7 +956,8 @@ constexpr int32_t kPrepParts = 512;
 
 template <int NB, class Op>
 __global__ __launch_bounds__(kPrepNT) void k_prep(Op op, int32_t n, int32_t m,
-                                                  float *__restrict__ part) {
+                                                  float *part0, float *part1,
+                                                  int64_t stride) {
   __shared__ float red[kPrepNT / kWave][kPrepCols][kVec];
   const int cg = threadIdx.x % kPrepCols, rg = threadIdx.x / kPrepCols;
   const int32_t col = ((int32_t)blockIdx.x * kPrepCols + cg) * kVec;
@@ -971,10 +974,11 @@ __global__ __launch_bounds__(kPrepNT) void k_prep(Op op, int32_t n, int32_t m,
       for (int p = 0; p < NB; ++p) sum[p] += v[p];
     }
   }
-  if (!part) return;
+  if (!part0 && !part1) return;
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
 #pragma unroll
   for (int p = 0; p < NB; ++p) {
+    float *part = p ? part1 : part0;
 #pragma unroll
     for (int i = 0; i < kVec; ++i) {
       sum[p][i] += __shfl_xor(sum[p][i], 16, kWave);
@@ -988,7 +992,7 @@ __global__ __launch_bounds__(kPrepNT) void k_prep(Op op, int32_t n, int32_t m,
       float t = 0.0f;
 #pragma unroll
       for (int w = 0; w < kPrepNT / kWave; ++w) t += red[w][c][i];
-      if (at < m) part[((int64_t)blockIdx.y * NB + p) * m + at] = t;
+      if (at < m && part) part[blockIdx.y * stride + at] = t;
     }
     __syncthreads();
   }
@@ -1003,11 +1007,14 @@ template <int NB, class Op>
 void prep_launch(const Op &op, int32_t n, int32_t m, float *part,
                  float *db0, float *db1, hipStream_t st) {
   const bool sums = db0 || db1;
-  const int32_t parts = prep_parts(n);
+  // a few steps of one block row cost less than a second launch
+  const int32_t parts = n <= 4 * kPrepRows && sums ? 1 : prep_parts(n);
+  const bool join = sums && parts > 1;
   const int32_t bx = (m + kPrepCols * kVec - 1) / (kPrepCols * kVec);
   hipLaunchKernelGGL((k_prep<NB, Op>), dim3((unsigned)bx, (unsigned)parts),
-                     dim3(kPrepNT), 0, st, op, n, m, sums ? part : nullptr);
-  if (sums) join_rows(part, parts, NB * m, db0, db1, m, st);
+                     dim3(kPrepNT), 0, st, op, n, m, join ? part : db0,
+                     join ? part + m : db1, (int64_t)NB * m);
+  if (join) join_rows(part, parts, NB * m, db0, db1, m, st);
 }
 
 // Bytes for the parts of a split product of m x n results: every part of a

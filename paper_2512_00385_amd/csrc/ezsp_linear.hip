@@ -50,19 +50,19 @@ struct NarrowLinear {
                                      Span s) const {
     Raw r;
     int32_t back;
-    r.dy = raw8(dy + span_at<TY>(row, lddy, n, d, s, back));
+    r.dy = raw8(dy + span_at(row, lddy, n, d, s, back));
     if constexpr (ACT)
-      r.z[0] = raw8(z + span_at<__bf16>(row, ldz, n, d, s, back));
+      r.z[0] = raw8(z + span_at(row, ldz, n, d, s, back));
     return r;
   }
   __device__ __forceinline__ void value(const Raw &r, int64_t row, int32_t n,
                                         int32_t d, Span s, f32x8_t *v) const {
     const int32_t cnt = row < n ? s.cnt : 0;
     int32_t back;
-    span_at<TY>(row, lddy, n, d, s, back);
+    span_at(row, lddy, n, d, s, back);
     v[0] = __builtin_convertvector(settle(r.dy, s.off + back, cnt), f32x8_t);
     if constexpr (ACT) {
-      span_at<__bf16>(row, ldz, n, d, s, back);
+      span_at(row, ldz, n, d, s, back);
       v[0] *= act_grad8(__builtin_convertvector(
                             settle(r.z[0], s.off + back, cnt), f32x8_t),
                         act);
@@ -88,8 +88,9 @@ void backward_narrow(const LinearArgs &a, hipStream_t st) {
   op.z = static_cast<const __bf16 *>(a.z);
   op.ldz = a.ldz;
   op.act = a.act;
-  narrow<NarrowLinear<TY, ACT>, 1>(g, op, static_cast<__bf16 *>(a.dw),
-                                   nullptr, a.db, nullptr, st);
+  g.dw[0] = static_cast<__bf16 *>(a.dw);
+  g.db[0] = a.db;
+  narrow<NarrowLinear<TY, ACT>, 1>(g, op, st);
 }
 
 // dz has to be formed unless dy is it already, at an alignment that the

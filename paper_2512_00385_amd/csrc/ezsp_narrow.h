@@ -90,89 +90,10 @@ struct NarrowArgs {
   int32_t n, d_in, d_out;
   __bf16 *dx;  // nullable
   int64_t lddx;
+  __bf16 *dw[2];  // nullable
+  float *db[2];   // nullable
   float *part;  // [block][product][d_in + 1][d_out]: dW, then db's row
 };
-
-// A lane's kVec columns from col on, of rows of d values.  They are loaded
-// without a branch, as they lie in memory: columns of an incomplete last
-// vector by way of the vector that ends with the row, rows past the end as
-// the last one.  settle() then shifts them into place and zeroes what does
-// not exist.  Rows shorter than a vector are loaded together with what
-// follows them, the table's last ones with what precedes them.
-struct Span {
-  int32_t at;   // column that the load starts at
-  int32_t cnt;  // columns that exist
-  int32_t off;  // first of them in the load
-  bool thin;    // d < kVec
-};
-__device__ __forceinline__ Span span_of(int32_t col, int32_t d) {
-  Span s;
-  s.cnt = min(max(d - col, 0), kVec);
-  s.at = min(col, max(d - kVec, 0));
-  s.off = col - s.at;
-  s.thin = d < kVec;
-  return s;
-}
-// rows [n] of the table and their distance; n * d >= kVec
-template <class T>
-__device__ __forceinline__ int64_t span_at(int64_t row, int64_t ld, int32_t n,
-                                           int32_t d, Span s, int32_t &back) {
-  const int64_t at = min(row, (int64_t)n - 1) * ld + s.at;
-  back = 0;
-  if (s.thin) {
-    const int64_t last = (int64_t)(n - 1) * ld + d - kVec;
-    if (at > last) back = (int32_t)(at - last);
-  }
-  return at - back;
-}
-template <class T>
-struct Vec8;  // kVec values in registers
-template <>
-struct Vec8<__bf16> {
-  u32x4_t v;
-};
-template <>
-struct Vec8<float> {
-  f32x8_t v;
-};
-__device__ __forceinline__ Vec8<__bf16> raw8(const __bf16 *p) {
-  return {*reinterpret_cast<const u32x4_u2 *>(p)};
-}
-__device__ __forceinline__ Vec8<float> raw8(const float *p) {
-  return {*reinterpret_cast<const f32x8_u *>(p)};
-}
-__device__ __forceinline__ bf16x8_t settle(Vec8<__bf16> r, int32_t off,
-                                           int32_t cnt) {
-  if (off) {
-    uint64_t lo = ((uint64_t)r.v[1] << 32) | r.v[0];
-    uint64_t hi = ((uint64_t)r.v[3] << 32) | r.v[2];
-    const int bits = 16 * off;  // those of 8 and more are zeroed below
-    lo = bits >= 64 ? hi >> (bits & 63)
-                    : (lo >> bits) | (hi << ((64 - bits) & 63));
-    hi = bits >= 64 ? 0 : hi >> bits;
-    r.v = u32x4_t{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi,
-                  (uint32_t)(hi >> 32)};
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    r.v[i] = cnt > 2 * i + 1 ? r.v[i] : cnt > 2 * i ? r.v[i] & 0xffffu : 0u;
-  return __builtin_bit_cast(bf16x8_t, r.v);
-}
-__device__ __forceinline__ f32x8_t settle(Vec8<float> r, int32_t off,
-                                          int32_t cnt) {
-  if (off) {
-#pragma unroll
-    for (int step = 4; step > 0; step >>= 1)
-      if (off & step) {
-#pragma unroll
-        for (int i = 0; i < kVec; ++i)
-          r.v[i] = i + step < kVec ? r.v[i + step] : 0.0f;
-      }
-  }
-#pragma unroll
-  for (int i = 0; i < kVec; ++i) r.v[i] = i < cnt ? r.v[i] : 0.0f;
-  return r.v;
-}
 
 // DT: 32-column tiles of x; CH chunks of COLS columns of dz per product, NB
 // products.  Op gives dz: raw() loads a row's columns, value() computes.
@@ -248,7 +169,7 @@ void k_narrow_bwd(NarrowArgs g,
 #pragma unroll
     for (int i = 0; i < kXLoads; ++i) {
       int32_t back;
-      xraw[i] = raw8(g.x + span_at<__bf16>(r0 + xr + i * (kNarrowNT / kXGroups),
+      xraw[i] = raw8(g.x + span_at(r0 + xr + i * (kNarrowNT / kXGroups),
                                            g.ldx, g.n, g.d_in, x_span, back));
     }
   };
@@ -270,7 +191,7 @@ void k_narrow_bwd(NarrowArgs g,
         {
           const int64_t row = r0 + xr + i * (kNarrowNT / kXGroups);
           int32_t back;
-          span_at<__bf16>(row, g.ldx, g.n, g.d_in, x_span, back);
+          span_at(row, g.ldx, g.n, g.d_in, x_span, back);
           X::put(xt, xr + i * (kNarrowNT / kXGroups), xc / kVec,
                  settle(xraw[i], x_span.off + back,
                         row < g.n ? x_span.cnt : 0));
@@ -354,8 +275,9 @@ void k_narrow_bwd(NarrowArgs g,
     }
   }
 
-  // this block's sums
-  const int64_t plane = (int64_t)(g.d_in + 1) * g.d_out;
+  // this block's sums: its parts, or the results where it is alone
+  const int64_t mat = (int64_t)g.d_in * g.d_out, plane = mat + g.d_out;
+  const bool alone = gridDim.x == 1;
   float *part = g.part + (int64_t)blockIdx.x * NB * plane;
 #pragma unroll
   for (int c = 0; c < CH; ++c)
@@ -371,8 +293,13 @@ void k_narrow_bwd(NarrowArgs g,
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             const int col = col0 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
-            if (d < g.d_in && col < g.d_out)
-              part[b * plane + (int64_t)d * g.d_out + col] = dw[c][j][i][r];
+            const int64_t at = (int64_t)d * g.d_out + col;
+            if (d < g.d_in && col < g.d_out) {
+              if (!alone)
+                part[b * plane + at] = dw[c][j][i][r];
+              else if (g.dw[b])
+                g.dw[b][at] = (__bf16)dw[c][j][i][r];
+            }
           }
         }
       }
@@ -390,10 +317,14 @@ void k_narrow_bwd(NarrowArgs g,
 #pragma unroll
       for (int i = 0; i < kVec; ++i) red[r_in * COLS + cg + i] = sum[c][b][i];
       __syncthreads();
-      if (tid < COLS && c * COLS + tid < g.d_out) {
+      const int col = c * COLS + tid;
+      if (tid < COLS && col < g.d_out) {
         float t = 0.0f;
         for (int r = 0; r < kStep; ++r) t += red[r * COLS + tid];
-        part[b * plane + (int64_t)g.d_in * g.d_out + c * COLS + tid] = t;
+        if (!alone)
+          part[b * plane + mat + col] = t;
+        else if (g.db[b])
+          g.db[b][col] = t;
       }
     }
 }
@@ -452,8 +383,7 @@ inline size_t narrow_part_bytes(int64_t n, int64_t d_in, int64_t d_out,
 }
 
 template <class Op, int NB, int DT, int COLS, int CH>
-void narrow_launch(const NarrowArgs &g, const Op &op, __bf16 *dw0,
-                   __bf16 *dw1, float *db0, float *db1, hipStream_t st) {
+void narrow_launch(const NarrowArgs &g, const Op &op, hipStream_t st) {
   static const int64_t slots = [] {
     int per_cu = 0;
     if (hipOccupancyMaxActiveBlocksPerMultiprocessor(
@@ -467,21 +397,20 @@ void narrow_launch(const NarrowArgs &g, const Op &op, __bf16 *dw0,
       ((int64_t)g.n + kNarrowRows - 1) / kNarrowRows, slots);
   hipLaunchKernelGGL((k_narrow_bwd<Op, NB, DT, COLS, CH>),
                      dim3((unsigned)blocks), dim3(kNarrowNT), 0, st, g, op);
-  if (!dw0 && !dw1 && !db0 && !db1) return;
+  if (blocks == 1 || (!g.dw[0] && !g.dw[1] && !g.db[0] && !g.db[1])) return;
   const int64_t len = (int64_t)NB * (g.d_in + 1) * g.d_out;
   hipLaunchKernelGGL(k_narrow_join<NB>,
                      dim3((unsigned)((len + kNJoinCols - 1) / kNJoinCols)),
                      dim3(kNJoinNT), 0, st, g.part, blocks, g.d_in, g.d_out,
-                     dw0, dw1, db0, db1);
+                     g.dw[0], g.dw[1], g.db[0], g.db[1]);
 }
 
 template <class Op, int NB>
-void narrow(const NarrowArgs &g, const Op &op, __bf16 *dw0, __bf16 *dw1,
-            float *db0, float *db1, hipStream_t st) {
+void narrow(const NarrowArgs &g, const Op &op, hipStream_t st) {
 #define EZSP_NARROW(DT, COLS, CH)                                         \
   do {                                                                    \
     if constexpr (DT * CH * NB <= 8 && CH * NB <= 4)                                    \
-      narrow_launch<Op, NB, DT, COLS, CH>(g, op, dw0, dw1, db0, db1, st); \
+      narrow_launch<Op, NB, DT, COLS, CH>(g, op, st);                     \
     return;                                                               \
   } while (0)
 #define EZSP_NARROW_D(DT)                       \

@@ -142,8 +142,10 @@ def test_backward(d, tx, ty):
         within(db, rdb, mb, F32, n / 16 + 64)
 
 
-@pytest.mark.parametrize("n,d", [(1, 5), (4099, 40), (50_001, 16),
-                                 (9001, 512)])
+@pytest.mark.parametrize("n,d", [(1, 5), (1, 1), (7, 1), (7, 3), (8, 1),
+                                 (9, 7), (4099, 40), (50_001, 16),
+                                 (9001, 512), (3001, 1500), (1100, 3001),
+                                 (1200, 6000)])
 def test_backward_rows(n, d):
     x, dy, _, _ = make(n, d, F32, F32, n)
     _, mean, rstd = forward64(x, None, None, EPS)
