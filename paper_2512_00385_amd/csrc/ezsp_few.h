@@ -225,7 +225,7 @@ __global__ __launch_bounds__(kFewNT) void k_few(GemmArgs<T> g, Epi epi) {
     const int row = it / (kCols / kVec);
     const int32_t col = n0 + it % (kCols / kVec) * kVec;
     if (it < kItems && row < g.m && col < g.n)
-      epi.apply(row, col, g.n - col, out[j]);
+      epi.at(epi.open(row, col, g.n), 0, out[j]);
   }
 }
 

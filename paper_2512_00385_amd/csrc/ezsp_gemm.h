@@ -123,6 +123,7 @@ struct Tile {
   uint32_t off[kCh];              // bytes from the tile's first element
   u32x4_t reg[FAST ? 1 : kCh];
   int32_t first, edge;            // !FAST: first row; rows left if not R
+  int32_t left;                   // k left of the step in reg
   bool slow, raw;                 // no vector fits a line; reg as loaded
 
   // where piece i of this thread comes from: (row, k) of its first element
@@ -162,6 +163,19 @@ struct Tile {
     }
   }
 
+  // How far back a K-major piece of the last step starts, in elements, so
+  // that it ends with the table at the latest (its last row ends after `left`
+  // more k).
+  __device__ __forceinline__ int32_t tail_back(int i, int32_t rows,
+                                               int64_t ld) const {
+    int r, k;
+    place(i, r, k);
+    r = min(r, rows - first - 1);
+    const int64_t over = (int64_t)(r - (rows - first - 1)) * ld + k + kPer -
+                         left;
+    return over > 0 ? (int32_t)over : 0;
+  }
+
   // Starts bringing in the tile whose first element is p; k_left counts the
   // k that exist from there on.
   __device__ __forceinline__ void fetch(const T *p, int64_t ld, int32_t rows,
@@ -195,6 +209,31 @@ struct Tile {
           reg[i] = *reinterpret_cast<const u32x4_u4 *>(src + off[i]);
       }
       raw = true;
+      left = kK;
+    } else if (!slow &&
+               (!KMAJOR || (int64_t)(rows - 1) * ld + k_left >= kPer)) {
+      // a last, incomplete step: pieces that would pass the table's end are
+      // taken from further back and shifted, lines past it repeat the last
+      // one; put() zeroes what lies past the end of k
+      left = k_left;
+      raw = true;
+#pragma unroll
+      for (int i = 0; i < kCh; ++i) {
+        int r, k;
+        place(i, r, k);
+        const T *q;
+        if constexpr (KMAJOR) {
+          r = min(r, rows - first - 1);
+          q = p + (int64_t)r * ld + k - tail_back(i, rows, ld);
+        } else {
+          q = p - first + (int64_t)min(k, k_left - 1) * ld +
+              min(first + r, rows - kPer);
+        }
+        if constexpr (sizeof(T) == 2)
+          reg[i] = *reinterpret_cast<const u32x4_u2 *>(q);
+        else
+          reg[i] = *reinterpret_cast<const u32x4_u4 *>(q);
+      }
     } else {
       const int32_t rows_left = rows - first;
 #pragma unroll
@@ -231,24 +270,36 @@ struct Tile {
   }
 
   // Ends it where the pieces went through registers.
-  __device__ __forceinline__ void put(char *lds) {
+  static __device__ __forceinline__ u32x4_t drop(u32x4_t v, int by) {
+    uint64_t lo = ((uint64_t)v[1] << 32) | v[0];
+    uint64_t hi = ((uint64_t)v[3] << 32) | v[2];
+    const int bits = min(by * (int)sizeof(T) * 8, 127);  // > 0
+    lo = bits >= 64 ? hi >> (bits & 63) : (lo >> bits) | (hi << (64 - bits));
+    hi = bits >= 64 ? 0 : hi >> bits;
+    return u32x4_t{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi,
+                   (uint32_t)(hi >> 32)};
+  }
+  __device__ __forceinline__ void put(char *lds, int32_t rows, int64_t ld) {
     if constexpr (!FAST) {
 #pragma unroll
       for (int i = 0; i < kCh; ++i) {
         u32x4_t v = reg[i];
-        if (!KMAJOR && raw && edge) {
+        if (raw && (left < kK || (!KMAJOR && edge))) {
           int r, k;
           place(i, r, k);
-          const int by = r - min(r, edge - kPer);  // elements
-          if (by > 0) {
-            uint64_t lo = ((uint64_t)v[1] << 32) | v[0];
-            uint64_t hi = ((uint64_t)v[3] << 32) | v[2];
-            const int bits = min(by * (int)sizeof(T) * 8, 127);
-            lo = bits >= 64 ? hi >> (bits & 63)
-                            : (lo >> bits) | (hi << (64 - bits));
-            hi = bits >= 64 ? 0 : hi >> bits;
-            v = u32x4_t{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi,
-                        (uint32_t)(hi >> 32)};
+          const int by = KMAJOR ? (left < kK ? tail_back(i, rows, ld) : 0)
+                         : edge ? r - min(r, edge - kPer)
+                                : 0;
+          if (by > 0) v = drop(v, by);
+          if (left < kK) {
+            const int cnt = KMAJOR ? left - k : k < left ? kPer : 0;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              if constexpr (sizeof(T) == 2)
+                v[q] = cnt > 2 * q + 1 ? v[q] : cnt > 2 * q ? v[q] & 0xffffu : 0u;
+              else
+                v[q] = cnt > q ? v[q] : 0u;
+            }
           }
         }
         *reinterpret_cast<u32x4_t *>(lds +
@@ -412,10 +463,10 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void k_gemm(
     }
   };
   auto put = [&](char *st) {
-    ta.put(st);
+    ta.put(st, g.ra, g.lda);
 #pragma unroll
     for (int p = 0; p < S::NB; ++p)
-      tb[p].put(st + S::TileA::kBytes + p * S::TileB::kBytes);
+      tb[p].put(st + S::TileA::kBytes + p * S::TileB::kBytes, g.rb, g.ldb);
   };
 
   f32x16_t acc[S::TM][S::TN];
@@ -490,6 +541,9 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void k_gemm(
                                  : 2 * S::kStage + (wave - S::kFit) * S::kOut));
     constexpr int kLanes = S::WC / kVec;  // lanes of a row
     const int32_t col = tile_n0 + wn * S::WC + (lane % kLanes) * kVec;
+    const int32_t row0 = tile_m0 + wm * S::TM * 32 + lane / kLanes;
+    const bool in_n = col < g.n;
+    const typename Epi::Lane view = epi.open(row0, in_n ? col : 0, g.n);
 #pragma unroll
     for (int i = 0; i < S::TM; ++i) {
 #pragma unroll
@@ -505,9 +559,10 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void k_gemm(
       __builtin_amdgcn_wave_barrier();
 #pragma unroll
       for (int pass = 0; pass < 32 * kLanes / kWave; ++pass) {
-        const int r = pass * (kWave / kLanes) + lane / kLanes;
-        const int32_t row = tile_m0 + (wm * S::TM + i) * 32 + r;
-        const float *src = out + r * S::kOutLd + (lane % kLanes) * kVec;
+        const int down = i * 32 + pass * (kWave / kLanes);
+        const float *src =
+            out + (pass * (kWave / kLanes) + lane / kLanes) * S::kOutLd +
+            (lane % kLanes) * kVec;
         f32x8_t v[S::NB];
 #pragma unroll
         for (int p = 0; p < S::NB; ++p) {
@@ -517,11 +572,11 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void k_gemm(
               *reinterpret_cast<const f32x4_t *>(src + p * S::WC + 4);
           v[p] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         }
-        if (row < g.m && col < g.n) {
+        if (row0 + down < g.m && in_n) {
           if (!g.to_parts)
-            epi.apply(row, col, g.n - col, v);
+            epi.at(view, down, v);
           else
-            epi.partial(tile_sp, g.m, g.n, row, col, v);
+            epi.partial(tile_sp, g.m, g.n, row0 + down, col, v);
         }
       }
       __builtin_amdgcn_wave_barrier();
@@ -596,11 +651,14 @@ __global__ __launch_bounds__(64 * SL) void k_gemm_join(int32_t splits,
         v[p] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
       }
     }
-    if (cnt > 0) epi.apply(row, col, cnt, v);
+    if (cnt > 0) epi.at(epi.open(row, col, n), 0, v);
   }
 }
 
 // --- epilogues --------------------------------------------------------------
+// open() gives a lane's view of kVec columns from col on, from a first row
+// on: the bias and where its results go; at() applies the epilogue `down` rows
+// further (uniform, so its addresses cost one addition).
 template <int NB>
 struct EpiParts {
   float *part;  // [split][product][m][n]
@@ -632,13 +690,28 @@ struct EpiLinear : EpiParts<1> {
     y = on(y, ldy, type_y);
     z = on(z, ldz, type);
   }
-  __device__ __forceinline__ void apply(int32_t row, int32_t col, int32_t cnt,
-                                        f32x8_t *v) const {
-    if (bias) v[0] += load8(bias + col, cnt);
-    if (z) store8_t(z, row * ldz + col, type, v[0], cnt);
+  struct Lane {
+    f32x8_t bias;
+    int64_t y, z, res;  // elements
+    int32_t cnt;
+  };
+  __device__ __forceinline__ Lane open(int64_t row, int32_t col,
+                                       int32_t n) const {
+    Lane l;
+    l.cnt = n - col;
+    l.bias = bias ? load8(bias + col, l.cnt) : f32x8_t(0.0f);
+    l.y = row * ldy + col;
+    l.z = row * ldz + col;
+    l.res = row * ldr + col;
+    return l;
+  }
+  __device__ __forceinline__ void at(const Lane &l, int64_t down,
+                                     f32x8_t *v) const {
+    v[0] += l.bias;
+    if (z) store8_t(z, l.z + down * ldz, type, v[0], l.cnt);
     f32x8_t o = act8(v[0], act);
-    if (res) o += load8_t(res, row * ldr + col, type_y, cnt);
-    store8_t(y, row * ldy + col, type_y, o, cnt);
+    if (res) o += load8_t(res, l.res + down * ldr, type_y, l.cnt);
+    store8_t(y, l.y + down * ldy, type_y, o, l.cnt);
   }
 };
 
@@ -654,14 +727,29 @@ struct EpiGated : EpiParts<2> {
     if (gate) gate += rows * lds;
     if (up) up += rows * lds;
   }
-  __device__ __forceinline__ void apply(int32_t row, int32_t col, int32_t cnt,
-                                        f32x8_t *v) const {
+  struct Lane {
+    f32x8_t bias[2];
+    int64_t h, s;
+    int32_t cnt;
+  };
+  __device__ __forceinline__ Lane open(int64_t row, int32_t col,
+                                       int32_t n) const {
+    Lane l;
+    l.cnt = n - col;
 #pragma unroll
     for (int p = 0; p < 2; ++p)
-      if (bias[p]) v[p] += load8(bias[p] + col, cnt);
-    if (gate) store8(gate + row * lds + col, v[0], cnt);
-    if (up) store8(up + row * lds + col, v[1], cnt);
-    store8(h + row * ldh + col, act8(v[0], act) * v[1], cnt);
+      l.bias[p] = bias[p] ? load8(bias[p] + col, l.cnt) : f32x8_t(0.0f);
+    l.h = row * ldh + col;
+    l.s = row * lds + col;
+    return l;
+  }
+  __device__ __forceinline__ void at(const Lane &l, int64_t down,
+                                     f32x8_t *v) const {
+    v[0] += l.bias[0];
+    v[1] += l.bias[1];
+    if (gate) store8(gate + l.s + down * lds, v[0], l.cnt);
+    if (up) store8(up + l.s + down * lds, v[1], l.cnt);
+    store8(h + l.h + down * ldh, act8(v[0], act) * v[1], l.cnt);
   }
 };
 
@@ -674,11 +762,19 @@ struct EpiStore : EpiParts<NB> {
     for (T *&o : out)
       if (o) o += rows * ld;
   }
-  __device__ __forceinline__ void apply(int32_t row, int32_t col, int32_t cnt,
-                                        f32x8_t *v) const {
+  struct Lane {
+    int64_t at;
+    int32_t cnt;
+  };
+  __device__ __forceinline__ Lane open(int64_t row, int32_t col,
+                                       int32_t n) const {
+    return {row * ld + col, n - col};
+  }
+  __device__ __forceinline__ void at(const Lane &l, int64_t down,
+                                     f32x8_t *v) const {
 #pragma unroll
     for (int p = 0; p < NB; ++p)
-      if (out[p]) store8(out[p] + row * ld + col, v[p], cnt);
+      if (out[p]) store8(out[p] + l.at + down * ld, v[p], l.cnt);
   }
 };
 
