@@ -828,50 +828,75 @@ int32_t gemm_launch(GemmArgs<typename S::T> g, const Epi &epi, int32_t splits,
   return g.splits;
 }
 
-// Splits of a sum over k for a product of `tiles` tiles: enough blocks to
-// fill the chip (two a CU, or one of the largest), eight steps a part at least
-// (a join costs what ten steps of a lone block do; four where 32 rows make a
-// step short: one token, 4096 -> 4096, takes 12.0 us in 16 parts and 13.5 in
-// 8), and no more parts than fit.
+// How a product is cut: its sum over k in `splits` parts, and the microseconds
+// that takes by the model below.
+struct Plan {
+  int32_t splits;
+  double us;
+};
+
+// The chip takes a launch's blocks in rounds of as many as its CUs hold.  A
+// step brings (BM + BN) lines of 128 bytes from L2, which gives a CU 55 bytes
+// a nanosecond when it holds one block and 69 when it holds more (17.7 TB/s in
+// all), and multiplies for 1.47 us per 256 x 256 tile in bfloat16, 0.95 per
+// 128 x 64 in fp32; the longer of the two counts.  So bfloat16 tiles of 128 x
+// 128 are bound by L2 (0.6 us a step alone, 0.94 for two) and only those of
+// 256 x 256 by the matrix cores.  Parts cost a second launch and 0.3 us a
+// megabyte.  (512 x 4096 -> 4096: 44.5 us in one part, 33.6 in two, 31.1 in
+// four, 42.3 in eight; 1024 x 1024 -> 1024: 12.9, 14.8 and 16.9 in one, two
+// and four.)
+//
+// With 32 rows or fewer the weights' bytes are what takes time: 512 blocks of
+// at least four steps (one token, 4096 -> 4096: 20.2 us in 4 parts, 13.5 in
+// 8, 12.0 in 16).
 template <class S>
-int32_t gemm_splits(const GemmArgs<typename S::T> &g, size_t part_bytes) {
+Plan gemm_plan(const GemmArgs<typename S::T> &g, size_t part_bytes) {
+  constexpr double kFetch = (S::BM + S::BN) * kLineBytes * 1e-3;  // KB
+  constexpr double kMul = sizeof(typename S::T) == 4
+                              ? 0.95 * S::BM * S::BN / (128 * 64)
+                              : 1.47 * S::BM * S::BN / (256 * 256);
+  constexpr int64_t per_cu = 160 * 1024 / S::kLds;
+  constexpr double one = std::max(kFetch / 55.0, kMul);
+  constexpr double full = per_cu * std::max(kFetch / 69.0, kMul);
   const int64_t tiles = (int64_t)((g.m + S::BM - 1) / S::BM) *
                         ((g.n + S::CN - 1) / S::CN);
   const int64_t kt = ((int64_t)g.k + S::kK - 1) / S::kK *
                      (S::MODE == kSeq ? 2 : 1);
-  const int64_t one = (int64_t)g.m * g.n * S::NB * 4;
-  const int64_t blocks = S::BM * S::BN >= 256 * 256 ? kCus : 2 * kCus;
-  int64_t s = std::min<int64_t>(blocks / std::max<int64_t>(tiles, 1),
-                                kt / (S::BM == 32 ? 4 : 8));
-  s = std::min<int64_t>(s, (int64_t)(part_bytes / (size_t)one));
-  return (int32_t)std::max<int64_t>(s, 1);
+  const double mat = 4.0 * g.m * g.n * S::NB;  // bytes of a part
+  const int64_t fit = (int64_t)((double)part_bytes / mat);
+  if (S::BM == 32) {
+    int64_t s = std::min<int64_t>(2 * kCus / std::max<int64_t>(tiles, 1),
+                                  kt / 4);
+    s = std::max<int64_t>(std::min(s, fit), 1);
+    return {(int32_t)s, 0.0};
+  }
+  Plan best = {1, 0.0};
+  for (int64_t s = 1; s <= 512; s += std::max<int64_t>(s / 4, 1)) {
+    if (s > 1 && (s > fit || s > kt / 4)) break;
+    const int64_t work = tiles * s, slots = per_cu * kCus;
+    const int64_t rest = work % slots;
+    const double round = (double)(work / slots) * full +
+                         (rest == 0      ? 0.0
+                          : rest <= kCus ? one
+                                         : full * ((rest + kCus - 1) / kCus) /
+                                               per_cu);
+    const double us = round * (double)((kt + s - 1) / s) +
+                      (s > 1 ? 4.0 + 0.3e-6 * mat * (double)s : 0.0);
+    if (s == 1 || us < best.us) best = {(int32_t)s, us};
+  }
+  return best;
 }
 
-// Time a step of a product in tiles of S, split as gemm_splits does: rounds
-// of per_cu blocks a CU at `full`, the last one at `one` where a block a CU is
-// enough for it.
-template <class S>
-double gemm_rounds(const GemmArgs<typename S::T> &g, size_t part_bytes,
-                   int per_cu, double one, double full) {
-  const int64_t splits = gemm_splits<S>(g, part_bytes);
-  const int64_t work = (int64_t)((g.m + S::BM - 1) / S::BM) *
-                       ((g.n + S::CN - 1) / S::CN) * splits;
-  const int64_t slots = per_cu * kCus;
-  const int64_t rest = work % slots;
-  return ((double)(work / slots) * full +
-          (rest == 0 ? 0.0 : rest <= kCus ? one : full)) /
-         (double)splits;
-}
-
-// Tile of the block by the shape of D; f gets its Shape.
+// Tile of the block by the shape of D; f gets its Shape and the splits.
 template <class T, bool AK, bool BK, int MODE, bool FAST, class F>
 void gemm_shape(const GemmArgs<T> &g, size_t part_bytes, F f) {
 #define EZSP_SHAPE(BM, BN, WM, WN) \
   Shape<T, BM, BN, WM, WN, AK, BK, MODE, FAST>
-#define EZSP_GEMM(BM, BN, WM, WN)      \
-  do {                                 \
-    f(EZSP_SHAPE(BM, BN, WM, WN){});   \
-    return;                            \
+#define EZSP_GEMM(BM, BN, WM, WN)                                         \
+  do {                                                                    \
+    typedef EZSP_SHAPE(BM, BN, WM, WN) S;                                 \
+    f(S{}, gemm_plan<S>(g, part_bytes).splits);                           \
+    return;                                                               \
   } while (0)
   constexpr int kB = MODE == kDual ? 2 : 1;
   if (g.m <= 32) EZSP_GEMM(32, 128, 1, kB == 2 ? 2 : 4);
@@ -886,13 +911,10 @@ void gemm_shape(const GemmArgs<T> &g, size_t part_bytes, F f) {
       EZSP_GEMM(128, 64, 2, 2);
   }
   if (g.n * kB <= 64) EZSP_GEMM(128, 64, 4, 1);
-  // microseconds a step: 1.47 for one 256 x 256 block a CU; 0.94 for two of
-  // 128 x 128, which hide each other's epilogues, 0.6 for one
   if constexpr (FAST && sizeof(T) == 2) {
     typedef EZSP_SHAPE(256, 256, 2, 4) L;
     typedef EZSP_SHAPE(128, 128, 2, 2) M;
-    if (gemm_rounds<L>(g, part_bytes, 1, 1.47, 1.47) <
-        gemm_rounds<M>(g, part_bytes, 2, 0.6, 0.94))
+    if (gemm_plan<L>(g, part_bytes).us < gemm_plan<M>(g, part_bytes).us)
       EZSP_GEMM(256, 256, 2, 4);
   }
   EZSP_GEMM(128, 128, 2, 2);
@@ -995,21 +1017,19 @@ void gemm(GemmArgs<T> g, Epi epi, size_t part_bytes, hipStream_t st) {
           for (int64_t r = 0; r < a_rows; r += chunk) {
             c.m = c.ra = (int32_t)std::min(chunk, a_rows - r);
             pack_launch(src + r * ld, ld, c.m, (int32_t)a_cols, dst, st);
-            gemm_shape<T, AK, BK, MODE, true>(c, room, [&](auto s) {
-              typedef decltype(s) S;
-              gemm_launch<S>(c, epi, gemm_splits<S>(c, room), false, st);
+            gemm_shape<T, AK, BK, MODE, true>(c, room, [&](auto s, int32_t sp) {
+              gemm_launch<decltype(s)>(c, epi, sp, false, st);
             });
             epi.shift(c.m);
           }
           return;
         }
         // chunks of the sum: their parts side by side, joined at the end
-        gemm_shape<T, AK, BK, MODE, true>(c, room, [&](auto s) {
+        gemm_shape<T, AK, BK, MODE, true>(g, room, [&](auto s, int32_t sp) {
           typedef decltype(s) S;
           const int64_t chunks = (a_rows + chunk - 1) / chunk;
           const size_t one = (size_t)g.m * g.n * S::NB * 4;
-          const int64_t all =
-              std::max<int64_t>(gemm_splits<S>(g, room), chunks);
+          const int64_t all = std::max<int64_t>(sp, chunks);
           const int64_t each = std::max<int64_t>(all / chunks, 1);
           if (room / one < (size_t)(each * chunks)) return;  // as they lie
           Epi at = epi;
@@ -1028,9 +1048,8 @@ void gemm(GemmArgs<T> g, Epi epi, size_t part_bytes, hipStream_t st) {
       }
     }
   }
-  auto whole = [&](auto s) {
-    typedef decltype(s) S;
-    gemm_launch<S>(g, epi, gemm_splits<S>(g, room), false, st);
+  auto whole = [&](auto s, int32_t sp) {
+    gemm_launch<decltype(s)>(g, epi, sp, false, st);
   };
   if (fast_a && fast_b)
     gemm_shape<T, AK, BK, MODE, true>(g, room, whole);
