@@ -83,27 +83,31 @@ __device__ __forceinline__ void store8(float *p, f32x8_t v, int cnt) {
 // the last one.  settle() then shifts them into place and zeroes what does
 // not exist.  Rows shorter than a vector are loaded together with what
 // follows them, the table's last ones with what precedes them.
-struct Span {
+template <int V>
+struct SpanOf {
   int32_t at;   // column that the load starts at
   int32_t cnt;  // columns that exist
   int32_t off;  // first of them in the load
-  bool thin;    // d < kVec
+  bool thin;    // d < V
 };
-__device__ __forceinline__ Span span_of(int32_t col, int32_t d) {
-  Span s;
-  s.cnt = min(max(d - col, 0), kVec);
-  s.at = min(col, max(d - kVec, 0));
+typedef SpanOf<kVec> Span;
+template <int V = kVec>
+__device__ __forceinline__ SpanOf<V> span_of(int32_t col, int32_t d) {
+  SpanOf<V> s;
+  s.cnt = min(max(d - col, 0), V);
+  s.at = min(col, max(d - V, 0));
   s.off = col - s.at;
-  s.thin = d < kVec;
+  s.thin = d < V;
   return s;
 }
-// rows [n] of the table and their distance; n * d >= kVec
+// rows [n] of the table and their distance; n * d >= V
+template <int V>
 __device__ __forceinline__ int64_t span_at(int64_t row, int64_t ld, int32_t n,
-                                           int32_t d, Span s, int32_t &back) {
+                                           int32_t d, SpanOf<V> s, int32_t &back) {
   const int64_t at = min(row, (int64_t)n - 1) * ld + s.at;
   back = 0;
   if (s.thin) {
-    const int64_t last = (int64_t)(n - 1) * ld + d - kVec;
+    const int64_t last = (int64_t)(n - 1) * ld + d - V;
     if (at > last) back = (int32_t)(at - last);
   }
   return at - back;

@@ -8,7 +8,7 @@
 // one product of twice the length, and both weights' gradients come from one
 // pass over x.  Few columns take the one-pass kernel instead.
 #include "ezsp_few.h"
-#include "ezsp_narrow.h"
+#include "ezsp_narrow_f32.h"
 
 namespace ezsp {
 
@@ -76,30 +76,68 @@ struct NarrowGated {
   }
 };
 
+// ... and for fp32, four columns at a time.
+struct NarrowGatedF32 {
+  const float *dh, *gate, *up;
+  int64_t lddh, lds;
+  int32_t act;
+  struct Raw {
+    f32x4_t d, g, u;
+  };
+  __device__ __forceinline__ Raw raw(int64_t row, int32_t n, int32_t d,
+                                     SpanOf<4> s) const {
+    Raw r;
+    int32_t back;
+    r.d = raw4(dh + span_at(row, lddh, n, d, s, back));
+    const int64_t at = span_at(row, lds, n, d, s, back);
+    r.g = raw4(gate + at);
+    r.u = raw4(up + at);
+    return r;
+  }
+  __device__ __forceinline__ void value(const Raw &r, int64_t row, int32_t n,
+                                        int32_t d, SpanOf<4> s,
+                                        f32x4_t *v) const {
+    const int32_t cnt = row < n ? s.cnt : 0;
+    int32_t back;
+    span_at(row, lds, n, d, s, back);
+    const f32x4_t u = settle4(r.u, s.off + back, cnt);
+    f32x8_t a, da;
+    act_both8(widen4(settle4(r.g, s.off + back, cnt)), act, a, da);
+    span_at(row, lddh, n, d, s, back);
+    const f32x4_t dv = settle4(r.d, s.off + back, cnt);
+    v[0] = dv * u * low4(da);
+    v[1] = dv * low4(a);
+  }
+};
+
+template <class T, class Op>
 void backward_narrow(const GatedArgs &a, hipStream_t st) {
-  NarrowArgs g = {};
-  g.x = static_cast<const __bf16 *>(a.x);
-  g.w[0] = static_cast<const __bf16 *>(a.w_gate);
-  g.w[1] = static_cast<const __bf16 *>(a.w_up);
+  NarrowArgs<T> g = {};
+  g.x = static_cast<const T *>(a.x);
+  g.w[0] = static_cast<const T *>(a.w_gate);
+  g.w[1] = static_cast<const T *>(a.w_up);
   g.ldx = a.ldx;
   g.n = a.n;
   g.d_in = a.d_in;
   g.d_out = a.d_out;
-  g.dx = static_cast<__bf16 *>(a.dx);
+  g.dx = static_cast<T *>(a.dx);
   g.lddx = a.lddx;
   g.part = a.part;
-  NarrowGated op;
-  op.dh = static_cast<const __bf16 *>(a.dh);
-  op.gate = static_cast<const __bf16 *>(a.gate);
-  op.up = static_cast<const __bf16 *>(a.up);
+  Op op;
+  op.dh = static_cast<const T *>(a.dh);
+  op.gate = static_cast<const T *>(a.gate);
+  op.up = static_cast<const T *>(a.up);
   op.lddh = a.lddh;
   op.lds = a.lds;
   op.act = a.act;
-  g.dw[0] = static_cast<__bf16 *>(a.dw_gate);
-  g.dw[1] = static_cast<__bf16 *>(a.dw_up);
+  g.dw[0] = static_cast<T *>(a.dw_gate);
+  g.dw[1] = static_cast<T *>(a.dw_up);
   g.db[0] = a.db_gate;
   g.db[1] = a.db_up;
-  narrow<NarrowGated, 2>(g, op, st);
+  if constexpr (sizeof(T) == 2)
+    narrow<Op, 2>(g, op, st);
+  else
+    narrow_f32<Op, 2>(g, op, st);
 }
 
 template <class T>
@@ -131,11 +169,12 @@ void forward(const GatedArgs &a, hipStream_t st) {
 
 template <class T>
 void backward(const GatedArgs &a, hipStream_t st) {
-  if constexpr (sizeof(T) == 2) {
-    if (narrow_fits(a.n, a.d_in, a.d_out, 2)) {
-      backward_narrow(a, st);
-      return;
-    }
+  if (narrow_serves(a.type, a.n, a.d_in, a.d_out, 2)) {
+    if constexpr (sizeof(T) == 2)
+      backward_narrow<T, NarrowGated>(a, st);
+    else
+      backward_narrow<T, NarrowGatedF32>(a, st);
+    return;
   }
   const int64_t half = pad_row(a.d_out);
   T *dz = static_cast<T *>(a.dz);
@@ -197,9 +236,8 @@ void gated_reserve(Arena &ar, int64_t n, int64_t d_in, int64_t d_out,
   a->part_bytes = gemm_part_bytes(d_in, n, d_out, 2);
   if (bwd) {
     // (sizes may not fall where the one-pass kernel starts to serve)
-    const int64_t rows = type == EZSP_TYPE_BF16 && narrow_fits(n, d_in, d_out, 2)
-                             ? kVec - 1
-                             : n;
+    const int64_t rows =
+        narrow_serves(type, n, d_in, d_out, 2) ? kVec - 1 : n;
     a->part_bytes = std::max(
         std::max(narrow_part_bytes(n, std::min<int64_t>(d_in, 128),
                                    std::min<int64_t>(d_out, 512), 2),

@@ -6,7 +6,7 @@
 // cores take it so, while db is summed from the unrounded values.  Few
 // columns take the one-pass kernel instead.
 #include "ezsp_few.h"
-#include "ezsp_narrow.h"
+#include "ezsp_narrow_f32.h"
 
 namespace ezsp {
 
@@ -70,27 +70,64 @@ struct NarrowLinear {
   }
 };
 
-template <class TY, bool ACT>
+// ... and for fp32, four columns at a time.
+template <bool ACT>
+struct NarrowLinearF32 {
+  const float *dy;
+  int64_t lddy;
+  const float *z;
+  int64_t ldz;
+  int32_t act;
+  struct Raw {
+    f32x4_t dy, z[ACT ? 1 : 0];
+  };
+  __device__ __forceinline__ Raw raw(int64_t row, int32_t n, int32_t d,
+                                     SpanOf<4> s) const {
+    Raw r;
+    int32_t back;
+    r.dy = raw4(dy + span_at(row, lddy, n, d, s, back));
+    if constexpr (ACT) r.z[0] = raw4(z + span_at(row, ldz, n, d, s, back));
+    return r;
+  }
+  __device__ __forceinline__ void value(const Raw &r, int64_t row, int32_t n,
+                                        int32_t d, SpanOf<4> s,
+                                        f32x4_t *v) const {
+    const int32_t cnt = row < n ? s.cnt : 0;
+    int32_t back;
+    span_at(row, lddy, n, d, s, back);
+    v[0] = settle4(r.dy, s.off + back, cnt);
+    if constexpr (ACT) {
+      span_at(row, ldz, n, d, s, back);
+      v[0] *= low4(
+          act_grad8(widen4(settle4(r.z[0], s.off + back, cnt)), act));
+    }
+  }
+};
+
+template <class T, class Op>
 void backward_narrow(const LinearArgs &a, hipStream_t st) {
-  NarrowArgs g = {};
-  g.x = static_cast<const __bf16 *>(a.x);
-  g.w[0] = g.w[1] = static_cast<const __bf16 *>(a.w);
+  NarrowArgs<T> g = {};
+  g.x = static_cast<const T *>(a.x);
+  g.w[0] = g.w[1] = static_cast<const T *>(a.w);
   g.ldx = a.ldx;
   g.n = a.n;
   g.d_in = a.d_in;
   g.d_out = a.d_out;
-  g.dx = static_cast<__bf16 *>(a.dx);
+  g.dx = static_cast<T *>(a.dx);
   g.lddx = a.lddx;
   g.part = a.part;
-  NarrowLinear<TY, ACT> op;
-  op.dy = static_cast<const TY *>(a.dy);
+  Op op;
+  op.dy = static_cast<decltype(op.dy)>(a.dy);
   op.lddy = a.lddy;
-  op.z = static_cast<const __bf16 *>(a.z);
+  op.z = static_cast<const T *>(a.z);
   op.ldz = a.ldz;
   op.act = a.act;
-  g.dw[0] = static_cast<__bf16 *>(a.dw);
+  g.dw[0] = static_cast<T *>(a.dw);
   g.db[0] = a.db;
-  narrow<NarrowLinear<TY, ACT>, 1>(g, op, st);
+  if constexpr (sizeof(T) == 2)
+    narrow<Op, 1>(g, op, st);
+  else
+    narrow_f32<Op, 1>(g, op, st);
 }
 
 // dz has to be formed unless dy is it already, at an alignment that the
@@ -130,17 +167,18 @@ void forward(const LinearArgs &a, hipStream_t st) {
 
 template <class T>
 void backward(const LinearArgs &a, hipStream_t st) {
-  if constexpr (sizeof(T) == 2) {
-    if (narrow_fits(a.n, a.d_in, a.d_out, 1)) {
-      const bool wide_y = a.type_y == EZSP_TYPE_F32;
-      if (a.act == EZSP_ACT_NONE)
-        wide_y ? backward_narrow<float, false>(a, st)
-               : backward_narrow<__bf16, false>(a, st);
-      else
-        wide_y ? backward_narrow<float, true>(a, st)
-               : backward_narrow<__bf16, true>(a, st);
-      return;
-    }
+  if (narrow_serves(a.type, a.n, a.d_in, a.d_out, 1)) {
+    const bool none = a.act == EZSP_ACT_NONE;
+    if constexpr (sizeof(T) == 4)
+      none ? backward_narrow<T, NarrowLinearF32<false>>(a, st)
+           : backward_narrow<T, NarrowLinearF32<true>>(a, st);
+    else if (a.type_y == EZSP_TYPE_F32)
+      none ? backward_narrow<T, NarrowLinear<float, false>>(a, st)
+           : backward_narrow<T, NarrowLinear<float, true>>(a, st);
+    else
+      none ? backward_narrow<T, NarrowLinear<__bf16, false>>(a, st)
+           : backward_narrow<T, NarrowLinear<__bf16, true>>(a, st);
+    return;
   }
   const bool form = needs_dz(a) && (a.dx || a.dw);
   const T *dz = static_cast<const T *>(a.dy);
@@ -201,9 +239,8 @@ void linear_reserve(Arena &ar, int64_t n, int64_t d_in, int64_t d_out,
   if (bwd) {
     // the one-pass kernel needs its parts alone, but sizes may not fall where
     // it starts to serve
-    const int64_t rows = type == EZSP_TYPE_BF16 && narrow_fits(n, d_in, d_out, 1)
-                             ? kVec - 1
-                             : n;
+    const int64_t rows =
+        narrow_serves(type, n, d_in, d_out, 1) ? kVec - 1 : n;
     a->part_bytes = std::max(
         std::max(narrow_part_bytes(n, std::min<int64_t>(d_in, 128),
                                    std::min<int64_t>(d_out, 512), 1),

@@ -84,13 +84,14 @@ struct NarrowTile {
   }
 };
 
+template <class T>
 struct NarrowArgs {
-  const __bf16 *x, *w[2];
+  const T *x, *w[2];
   int64_t ldx;
   int32_t n, d_in, d_out;
-  __bf16 *dx;  // nullable
+  T *dx;  // nullable
   int64_t lddx;
-  __bf16 *dw[2];  // nullable
+  T *dw[2];     // nullable
   float *db[2];   // nullable
   float *part;  // [block][product][d_in + 1][d_out]: dW, then db's row
 };
@@ -105,8 +106,7 @@ constexpr int narrow_waves(int nb, int dt, int cols, int ch) {
 
 template <class Op, int NB, int DT, int COLS, int CH>
 __global__ __launch_bounds__(kNarrowNT, narrow_waves(NB, DT, COLS, CH))
-void k_narrow_bwd(NarrowArgs g,
-                                                          Op op) {
+void k_narrow_bwd(NarrowArgs<__bf16> g, Op op) {
   constexpr int kDzBytes = NB * COLS * 2;       // a row of the dz tile
   constexpr int kWBytes = NB * COLS * CH * 2;   // a row of W: all of dz's
   constexpr int kXBytes = DT * 64;
@@ -332,10 +332,10 @@ void k_narrow_bwd(NarrowArgs g,
 // Adds the blocks' sums in order: part[block][product][d_in + 1][d_out].
 constexpr int kNJoinCols = 32;
 constexpr int kNJoinNT = 1024;
-template <int NB>
+template <class T, int NB>
 __global__ __launch_bounds__(kNJoinNT) void k_narrow_join(
     const float *__restrict__ part, int32_t parts, int32_t d_in,
-    int32_t d_out, __bf16 *dw0, __bf16 *dw1, float *db0, float *db1) {
+    int32_t d_out, T *dw0, T *dw1, float *db0, float *db1) {
   constexpr int kSlices = kNJoinNT / kNJoinCols;
   __shared__ float sl[kSlices][kNJoinCols];
   const int64_t plane = (int64_t)(d_in + 1) * d_out, len = NB * plane;
@@ -354,14 +354,24 @@ __global__ __launch_bounds__(kNJoinNT) void k_narrow_join(
     for (int t = 0; t < kSlices; ++t) v += sl[t][c];
     const int b = at >= plane;
     const int64_t e = at - b * plane, mat = (int64_t)d_in * d_out;
-    __bf16 *dw = b ? dw1 : dw0;
+    T *dw = b ? dw1 : dw0;
     float *db = b ? db1 : db0;
     if (e < mat) {
-      if (dw) dw[e] = (__bf16)v;
+      if (dw) dw[e] = (T)v;
     } else if (db) {
       db[e - mat] = v;
     }
   }
+}
+
+template <class T, int NB>
+void narrow_join(const NarrowArgs<T> &g, int32_t blocks, hipStream_t st) {
+  if (blocks == 1 || (!g.dw[0] && !g.dw[1] && !g.db[0] && !g.db[1])) return;
+  const int64_t len = (int64_t)NB * (g.d_in + 1) * g.d_out;
+  hipLaunchKernelGGL((k_narrow_join<T, NB>),
+                     dim3((unsigned)((len + kNJoinCols - 1) / kNJoinCols)),
+                     dim3(kNJoinNT), 0, st, g.part, blocks, g.d_in, g.d_out,
+                     g.dw[0], g.dw[1], g.db[0], g.db[1]);
 }
 
 // Whether a block's registers and LDS hold the weights and their sums:
@@ -383,7 +393,7 @@ inline size_t narrow_part_bytes(int64_t n, int64_t d_in, int64_t d_out,
 }
 
 template <class Op, int NB, int DT, int COLS, int CH>
-void narrow_launch(const NarrowArgs &g, const Op &op, hipStream_t st) {
+void narrow_launch(const NarrowArgs<__bf16> &g, const Op &op, hipStream_t st) {
   static const int64_t slots = [] {
     int per_cu = 0;
     if (hipOccupancyMaxActiveBlocksPerMultiprocessor(
@@ -397,19 +407,14 @@ void narrow_launch(const NarrowArgs &g, const Op &op, hipStream_t st) {
       ((int64_t)g.n + kNarrowRows - 1) / kNarrowRows, slots);
   hipLaunchKernelGGL((k_narrow_bwd<Op, NB, DT, COLS, CH>),
                      dim3((unsigned)blocks), dim3(kNarrowNT), 0, st, g, op);
-  if (blocks == 1 || (!g.dw[0] && !g.dw[1] && !g.db[0] && !g.db[1])) return;
-  const int64_t len = (int64_t)NB * (g.d_in + 1) * g.d_out;
-  hipLaunchKernelGGL(k_narrow_join<NB>,
-                     dim3((unsigned)((len + kNJoinCols - 1) / kNJoinCols)),
-                     dim3(kNJoinNT), 0, st, g.part, blocks, g.d_in, g.d_out,
-                     g.dw[0], g.dw[1], g.db[0], g.db[1]);
+  narrow_join<__bf16, NB>(g, blocks, st);
 }
 
 template <class Op, int NB>
-void narrow(const NarrowArgs &g, const Op &op, hipStream_t st) {
+void narrow(const NarrowArgs<__bf16> &g, const Op &op, hipStream_t st) {
 #define EZSP_NARROW(DT, COLS, CH)                                         \
   do {                                                                    \
-    if constexpr (DT * CH * NB <= 8 && CH * NB <= 4)                                    \
+    if constexpr (DT * CH * NB <= 8 && CH * NB <= 4)                      \
       narrow_launch<Op, NB, DT, COLS, CH>(g, op, st);                     \
     return;                                                               \
   } while (0)
