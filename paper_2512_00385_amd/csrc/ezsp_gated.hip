@@ -9,6 +9,7 @@
 // pass over x.  Few columns take the one-pass kernel instead.
 #include "ezsp_few.h"
 #include "ezsp_narrow_f32.h"
+#include "ezsp_narrow_fwd.h"
 
 namespace ezsp {
 
@@ -163,6 +164,8 @@ void forward(const GatedArgs &a, hipStream_t st) {
   e.act = a.act;
   if (few_serves(g, 2))
     few<T, 2>(g, e, st);
+  else if (narrow_fwd_serves(g))
+    narrow_fwd<T, 2>(g, e, st);
   else
     gemm<T, true, false, kDual>(g, e, a.part_bytes, st);
 }

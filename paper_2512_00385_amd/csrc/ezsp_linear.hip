@@ -7,6 +7,7 @@
 // columns take the one-pass kernel instead.
 #include "ezsp_few.h"
 #include "ezsp_narrow_f32.h"
+#include "ezsp_narrow_fwd.h"
 
 namespace ezsp {
 
@@ -161,6 +162,8 @@ void forward(const LinearArgs &a, hipStream_t st) {
   e.act = a.act;
   if (few_serves(g, 1))
     few<T, 1>(g, e, st);
+  else if (narrow_fwd_serves(g))
+    narrow_fwd<T, 1>(g, e, st);
   else
     gemm<T, true, false, kPlain>(g, e, a.part_bytes, st);
 }

@@ -1,4 +1,4 @@
-"""The one-pass backward of products over many rows with few columns, in the
+"""Products over many rows with few columns, both directions, in the
 widths where its tiles change, on integers: sums of products of small integers
 are exact in fp32 in any order, so results are compared for equality with
 64-bit ones (dW and dx in bfloat16 after one rounding).  The tables lie in
@@ -94,3 +94,35 @@ def test_results_alone_match_all(ty):
         for j in range(3):
             assert (got[j] is None) == (not want[j])
         assert torch.equal(got[i], full[i])
+
+
+@pytest.mark.parametrize("ty", [F32, BF])
+@pytest.mark.parametrize("k,m", [(1, 1), (3, 7), (6, 4), (7, 33), (8, 16),
+                                 (15, 17), (16, 32), (16, 33), (17, 8),
+                                 (31, 64), (32, 63), (33, 65)])
+def test_forward(k, m, ty):
+    for i, n in enumerate((8, 1023, 1024, 1055, 1153, 9000)):
+        g = torch.Generator().manual_seed(n + k + m)
+        pad = (0, 1, 8)[i % 3]
+        x, res = (inset(ints(g, (n, d), 2, ty), pad) for d in (k, m))
+        w = [ints(g, (k, m), 2, ty) for _ in range(2)]
+        b = [ints(g, (m,), 5, F32) for _ in range(2)]
+        s = [x.double() @ wi.double() + bi.double() for wi, bi in zip(w, b)]
+        y, z = ezsp.linear(x, w[0], b[0], "relu", res, want_z=True)
+        assert torch.equal(z, s[0].to(ty)), (n, pad)
+        assert torch.equal(y, (s[0].clamp_min(0) + res.double()).to(ty))
+        h, gate, up = ezsp.gated_ff(x, *w, *b, act="relu", want_saved=True)
+        assert torch.equal(gate, s[0].to(ty)) and torch.equal(up, s[1].to(ty))
+        assert torch.equal(h, (s[0].clamp_min(0) * s[1]).to(ty)), (n, pad)
+        assert torch.equal(ezsp.gated_ff(x, *w, *b, act="relu"), h)
+
+
+@pytest.mark.parametrize("ty", [F32, BF])
+def test_forward_keeps_rows_apart(ty):
+    g = torch.Generator().manual_seed(2)
+    x, w = ints(g, (3000, 6), 2, ty), ints(g, (6, 12), 2, ty)
+    ref = ezsp.linear(x, w)
+    x[1500] = float("nan")
+    y = ezsp.linear(x, w)
+    keep = torch.arange(3000) != 1500
+    assert torch.equal(y[keep], ref[keep]) and torch.isnan(y[1500]).all()
