@@ -22,9 +22,9 @@
  *   - `stream` is a hipStream_t passed as void* (NULL = the null stream).
  *     All device work is enqueued on it.
  *   - ezsp_knn, ezsp_component_stats, ezsp_embed_mlp and the dense operators
- *     (ezsp_layer_norm and after) are stream-asynchronous: they validate their arguments, enqueue their
- *     kernels and return; their outputs are ready once `stream` reaches
- *     that point, and their workspace must stay allocated until then.
+ *     (ezsp_layer_norm and after) are stream-asynchronous: they validate
+ *     their arguments, enqueue their kernels and return; their outputs are
+ *     ready once `stream` reaches that point, and their workspace must stay allocated until then.
  *     Errors the device detects (a non-finite coordinate, a label out of
  *     range) are kept in the call's workspace and reported by
  *     ezsp_sync_status.  The entry points that return host values
