@@ -441,6 +441,14 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void k_gemm(
 #pragma unroll
     for (int p = 0; p < S::NB; ++p) tb[p].init(n0, g.rb, g.ldb);
   };
+  // After a tile's last step, the block's next tile.  A step that goes by way
+  // of registers is finished by put() with what init() and fetch() noted of
+  // its tile, so there the next one opens after that.
+  auto advance = [&] {
+    if (f_t < f_end) return;
+    f_blk += gridDim.x;
+    if (f_blk < total) open();
+  };
   auto fetch = [&](char *st) {
     if (f_blk >= total) return;
     const bool second = S::MODE == kSeq && f_t >= kt1;
@@ -457,16 +465,17 @@ __global__ __launch_bounds__(S::NT, S::kWaves) void k_gemm(
                   g.ldb, g.rb, g.kb - k0,
                   st + S::TileA::kBytes + p * S::TileB::kBytes);
     }
-    if (++f_t == f_end) {
-      f_blk += gridDim.x;
-      if (f_blk < total) open();
-    }
+    ++f_t;
+    if (S::FAST) advance();
   };
+  // every fetch() has its put() before the next one
   auto put = [&](char *st) {
+    if (S::FAST) return;
     ta.put(st, g.ra, g.lda);
 #pragma unroll
     for (int p = 0; p < S::NB; ++p)
       tb[p].put(st + S::TileA::kBytes + p * S::TileB::kBytes, g.rb, g.ldb);
+    advance();
   };
 
   f32x16_t acc[S::TM][S::TN];
