@@ -55,7 +55,8 @@ __global__ __launch_bounds__(kFewNT) void k_few(GemmArgs<T> g, Epi epi) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int grp = lane >> 4;
   // a last, incomplete vector is the one that ends with the row of W: its
-  // columns are then computed twice, alike
+  // columns are then computed twice, alike, those before the block's first
+  // for nothing
   const int32_t n0 = (int32_t)blockIdx.x * kCols;
   const int32_t at = min(n0 + V * (lane & 15), g.n - V);
 
@@ -203,7 +204,8 @@ __global__ __launch_bounds__(kFewNT) void k_few(GemmArgs<T> g, Epi epi) {
       for (int v = 0; v < V; ++v)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          part[wave][16 * m + 4 * grp + r][at - n0 + v] = acc[b][m][v][r];
+          if (at + v >= n0)
+            part[wave][16 * m + 4 * grp + r][at - n0 + v] = acc[b][m][v][r];
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
