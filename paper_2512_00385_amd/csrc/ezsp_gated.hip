@@ -130,7 +130,7 @@ void backward_narrow(const GatedArgs &a, hipStream_t st) {
   op.up = static_cast<const T *>(a.up);
   op.lddh = a.lddh;
   op.lds = a.lds;
-  op.act = a.act;
+  op.act = act_for(a.act, a.type);
   g.dw[0] = static_cast<T *>(a.dw_gate);
   g.dw[1] = static_cast<T *>(a.dw_up);
   g.db[0] = a.db_gate;
@@ -161,7 +161,7 @@ void forward(const GatedArgs &a, hipStream_t st) {
   e.gate = static_cast<T *>(a.gate);
   e.up = static_cast<T *>(a.up);
   e.lds = a.lds;
-  e.act = a.act;
+  e.act = act_for(a.act, a.type);
   if (few_serves(g, 2))
     few<T, 2>(g, e, st);
   else if (narrow_fwd_serves(g))
@@ -188,7 +188,7 @@ void backward(const GatedArgs &a, hipStream_t st) {
     p.gate = static_cast<const T *>(a.gate);
     p.up = static_cast<const T *>(a.up);
     p.lds = a.lds;
-    p.act = a.act;
+    p.act = act_for(a.act, a.type);
     p.dz = a.dx || a.dw_gate || a.dw_up ? dz : nullptr;
     p.lddz = 2 * half;
     p.half = half;

@@ -122,7 +122,7 @@ void backward_narrow(const LinearArgs &a, hipStream_t st) {
   op.lddy = a.lddy;
   op.z = static_cast<const T *>(a.z);
   op.ldz = a.ldz;
-  op.act = a.act;
+  op.act = act_for(a.act, a.type);
   g.dw[0] = static_cast<T *>(a.dw);
   g.db[0] = a.db;
   if constexpr (sizeof(T) == 2)
@@ -159,7 +159,7 @@ void forward(const LinearArgs &a, hipStream_t st) {
   e.ldz = a.ldz;
   e.type = a.type;
   e.type_y = a.type_y;
-  e.act = a.act;
+  e.act = act_for(a.act, a.type_y);
   if (few_serves(g, 1))
     few<T, 1>(g, e, st);
   else if (narrow_fwd_serves(g))
@@ -193,7 +193,7 @@ void backward(const LinearArgs &a, hipStream_t st) {
     p.type_y = a.type_y;
     p.z = static_cast<const T *>(a.z);
     p.ldz = a.ldz;
-    p.act = a.act;
+    p.act = act_for(a.act, a.type);
     p.dz = form ? static_cast<T *>(a.dz) : nullptr;
     p.lddz = pad_row(a.d_out);
     prep_launch<1>(p, a.n, a.d_out, a.part, a.db, nullptr, st);
