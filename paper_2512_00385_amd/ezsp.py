@@ -519,12 +519,20 @@ TYPE_CODES = {torch.bfloat16: 0, torch.float32: 1}
 ACT_CODES = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 
 
+def _on_device(t, name, like=None):
+    """Checks that t is a device tensor, with `like` on the same device."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a device tensor")
+    if like is not None and t.get_device() != like.get_device():
+        raise ValueError(f"{name} must be on device {like.get_device()} as "
+                         f"x, is on {t.get_device()}")
+
+
 def _rows(t, name, like=None, cols=None, dtype=None):
     """A [n, d] device tensor whose rows are contiguous (columns of a wider
     table stay as they are, other orders are copied) and the distance
-    between its rows."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise TypeError(f"{name} must be a device tensor")
+    between its rows; with `like` it has as many rows, on its device."""
+    _on_device(t, name, like)
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if t.dtype not in TYPE_CODES:
@@ -532,9 +540,9 @@ def _rows(t, name, like=None, cols=None, dtype=None):
     if t.dim() != 2:
         raise ValueError(f"{name} must have shape [n, d]")
     n, d = t.shape
-    if like is not None and (n != like or d != cols):
-        raise ValueError(f"{name} must have shape [{like}, {cols}], got "
-                         f"{list(t.shape)}")
+    if like is not None and (n != like.shape[0] or d != cols):
+        raise ValueError(f"{name} must have shape [{like.shape[0]}, {cols}], "
+                         f"got {list(t.shape)}")
     ld, one = t.stride()
     if (one != 1 and d > 1) or (ld < d and n > 1):
         t = t.contiguous()
@@ -542,12 +550,11 @@ def _rows(t, name, like=None, cols=None, dtype=None):
     return t, max(ld, d)
 
 
-def _vector(t, d, name):
-    """A contiguous fp32 device vector of d values, or None."""
+def _vector(t, d, name, like):
+    """A contiguous fp32 vector of d values on like's device, or None."""
     if t is None:
         return None
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise TypeError(f"{name} must be a device tensor")
+    _on_device(t, name, like)
     if t.dtype != torch.float32:
         raise TypeError(f"{name} must be torch.float32, got {t.dtype}")
     if t.shape != (d,):
@@ -587,7 +594,7 @@ def layer_norm(x: torch.Tensor, weight=None, bias=None, eps: float = 1e-5,
     lib = load()
     x, ldx = _rows(x, "x")
     n, d = x.shape
-    weight, bias = _vector(weight, d, "weight"), _vector(bias, d, "bias")
+    weight, bias = _vector(weight, d, "weight", x), _vector(bias, d, "bias", x)
     out_dtype = out_dtype or x.dtype
     if out_dtype not in TYPE_CODES:
         raise TypeError("out_dtype must be bfloat16 or float32")
@@ -613,12 +620,12 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor,
     lib = load()
     x, ldx = _rows(x, "x")
     n, d = x.shape
-    dy, lddy = _rows(dy, "dy", n, d)
-    mean, rstd = _vector(mean, n, "mean"), _vector(rstd, n, "rstd")
-    weight = _vector(weight, d, "weight")
+    dy, lddy = _rows(dy, "dy", x, d)
+    mean, rstd = _vector(mean, n, "mean", x), _vector(rstd, n, "rstd", x)
+    weight = _vector(weight, d, "weight", x)
     lddres = 0
     if dres is not None:
-        dres, lddres = _rows(dres, "dres", n, d, x.dtype)
+        dres, lddres = _rows(dres, "dres", x, d, x.dtype)
     dev = x.device
     dx = torch.empty((n, d), dtype=x.dtype, device=dev) if want_dx else None
     dw = db = None
@@ -635,15 +642,14 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor,
     return dx, dw, db
 
 
-def _weight(t, d_in, dtype, name, d_out=None):
-    """A contiguous device matrix [d_in, d_out] of the given type."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise TypeError(f"{name} must be a device tensor")
-    if t.dtype != dtype:
-        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-    if t.dim() != 2 or t.shape[0] != d_in or \
+def _weight(t, x, name, d_out=None):
+    """A contiguous matrix [d_in, d_out] of x's type, on its device."""
+    _on_device(t, name, x)
+    if t.dtype != x.dtype:
+        raise TypeError(f"{name} must be {x.dtype}, got {t.dtype}")
+    if t.dim() != 2 or t.shape[0] != x.shape[1] or \
             (d_out is not None and t.shape[1] != d_out):
-        raise ValueError(f"{name} must have shape [{d_in}, "
+        raise ValueError(f"{name} must have shape [{x.shape[1]}, "
                          f"{'d_out' if d_out is None else d_out}]")
     return t.contiguous()
 
@@ -665,16 +671,16 @@ def linear(x: torch.Tensor, w: torch.Tensor, bias=None, act: str = "none",
     x, ldx = _rows(x, "x")
     n, d_in = x.shape
     ty, dev = x.dtype, x.device
-    w = _weight(w, d_in, ty, "w")
+    w = _weight(w, x, "w")
     d_out = w.shape[1]
     code = _act(act)
-    bias = _vector(bias, d_out, "bias")
+    bias = _vector(bias, d_out, "bias", x)
     out_dtype = out_dtype or ty
     if out_dtype not in (ty, torch.float32):
         raise TypeError("out_dtype must be x's type or float32")
     ldr = 0
     if residual is not None:
-        residual, ldr = _rows(residual, "residual", n, d_out, out_dtype)
+        residual, ldr = _rows(residual, "residual", x, d_out, out_dtype)
     y = torch.empty((n, d_out), dtype=out_dtype, device=dev)
     z = torch.empty((n, d_out), dtype=ty, device=dev) if want_z else None
     nbytes = _dense_bytes("ezsp_linear_workspace_size", n, d_in, d_out)
@@ -698,13 +704,13 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor,
     x, ldx = _rows(x, "x")
     n, d_in = x.shape
     ty, dev = x.dtype, x.device
-    w = _weight(w, d_in, ty, "w")
+    w = _weight(w, x, "w")
     d_out = w.shape[1]
     code = _act(act)
-    dy, lddy = _rows(dy, "dy", n, d_out)
+    dy, lddy = _rows(dy, "dy", x, d_out)
     ldz = 0
     if z is not None:
-        z, ldz = _rows(z, "z", n, d_out, ty)
+        z, ldz = _rows(z, "z", x, d_out, ty)
     dx = torch.empty((n, d_in), dtype=ty, device=dev) if want_dx else None
     dw = torch.empty((d_in, d_out), dtype=ty, device=dev) if want_dw else None
     db = torch.empty(d_out, dtype=torch.float32, device=dev) \
@@ -732,12 +738,12 @@ def gated_ff(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor,
     x, ldx = _rows(x, "x")
     n, d_in = x.shape
     ty, dev = x.dtype, x.device
-    w_gate = _weight(w_gate, d_in, ty, "w_gate")
+    w_gate = _weight(w_gate, x, "w_gate")
     d_out = w_gate.shape[1]
-    w_up = _weight(w_up, d_in, ty, "w_up", d_out)
+    w_up = _weight(w_up, x, "w_up", d_out)
     code = _act(act)
-    b_gate = _vector(b_gate, d_out, "b_gate")
-    b_up = _vector(b_up, d_out, "b_up")
+    b_gate = _vector(b_gate, d_out, "b_gate", x)
+    b_up = _vector(b_up, d_out, "b_up", x)
     h = torch.empty((n, d_out), dtype=ty, device=dev)
     gate = up = None
     if want_saved:
@@ -765,13 +771,13 @@ def gated_ff_backward(dh: torch.Tensor, x: torch.Tensor,
     x, ldx = _rows(x, "x")
     n, d_in = x.shape
     ty, dev = x.dtype, x.device
-    w_gate = _weight(w_gate, d_in, ty, "w_gate")
+    w_gate = _weight(w_gate, x, "w_gate")
     d_out = w_gate.shape[1]
-    w_up = _weight(w_up, d_in, ty, "w_up", d_out)
+    w_up = _weight(w_up, x, "w_up", d_out)
     code = _act(act)
-    dh, lddh = _rows(dh, "dh", n, d_out, ty)
-    gate, lds = _rows(gate, "gate", n, d_out, ty)
-    up, lds_up = _rows(up, "up", n, d_out, ty)
+    dh, lddh = _rows(dh, "dh", x, d_out, ty)
+    gate, lds = _rows(gate, "gate", x, d_out, ty)
+    up, lds_up = _rows(up, "up", x, d_out, ty)
     if lds != lds_up:
         gate, up, lds = gate.contiguous(), up.contiguous(), d_out
     dx = torch.empty((n, d_in), dtype=ty, device=dev) if want_dx else None
