@@ -519,11 +519,12 @@ TYPE_CODES = {torch.bfloat16: 0, torch.float32: 1}
 ACT_CODES = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 
 
-def _on_device(t, name, like=None):
-    """Checks that t is a device tensor, with `like` on the same device."""
+def _elsewhere(t, name, like):
+    """Raises for a t that is not a tensor on like's device (any device
+    without)."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a device tensor")
-    if like is not None and t.get_device() != like.get_device():
+    if like is not None:
         raise ValueError(f"{name} must be on device {like.get_device()} as "
                          f"x, is on {t.get_device()}")
 
@@ -532,7 +533,9 @@ def _rows(t, name, like=None, cols=None, dtype=None):
     """A [n, d] device tensor whose rows are contiguous (columns of a wider
     table stay as they are, other orders are copied) and the distance
     between its rows; with `like` it has as many rows, on its device."""
-    _on_device(t, name, like)
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or \
+            (like is not None and t.get_device() != like.get_device()):
+        _elsewhere(t, name, like)
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if t.dtype not in TYPE_CODES:
@@ -554,7 +557,9 @@ def _vector(t, d, name, like):
     """A contiguous fp32 vector of d values on like's device, or None."""
     if t is None:
         return None
-    _on_device(t, name, like)
+    if not isinstance(t, torch.Tensor) or \
+            t.get_device() != like.get_device():
+        _elsewhere(t, name, like)
     if t.dtype != torch.float32:
         raise TypeError(f"{name} must be torch.float32, got {t.dtype}")
     if t.shape != (d,):
@@ -585,6 +590,22 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
     (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or \
+    torch.cuda.current_device
+
+
+def _on(device, fn):
+    """fn, called with the device made the current one: a default stream is
+    the current device's, whatever device it was asked of."""
+    if device.index == _current_device():
+        return fn
+
+    def call(*args):
+        with torch.cuda.device(device):
+            return fn(*args)
+    return call
+
+
 def layer_norm(x: torch.Tensor, weight=None, bias=None, eps: float = 1e-5,
                out_dtype=None, want_stats: bool = False):
     """Layer norm over each row of x [n, d] (ezsp_layer_norm), bfloat16 or
@@ -603,10 +624,11 @@ def layer_norm(x: torch.Tensor, weight=None, bias=None, eps: float = 1e-5,
     if want_stats:
         mean = torch.empty(n, dtype=torch.float32, device=x.device)
         rstd = torch.empty(n, dtype=torch.float32, device=x.device)
-    _check(lib.ezsp_layer_norm(
+    _check(_on(x.device, lib.ezsp_layer_norm)(
         x.data_ptr(), ldx, TYPE_CODES[x.dtype], n, d, _at(weight), _at(bias),
         float(eps), y.data_ptr(), d, TYPE_CODES[out_dtype], _at(mean),
-        _at(rstd), _raw_stream(x.device.index)), "ezsp_layer_norm")
+        _at(rstd),
+        _raw_stream(x.device.index)), "ezsp_layer_norm")
     return (y, mean, rstd) if want_stats else y
 
 
@@ -634,17 +656,19 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor,
         db = torch.empty(d, dtype=torch.float32, device=dev)
     nbytes = _dense_bytes("ezsp_layer_norm_backward_workspace_size", n, d)
     ws = _dense_ws(nbytes, dev)
-    _check(lib.ezsp_layer_norm_backward(
+    _check(_on(dev, lib.ezsp_layer_norm_backward)(
         dy.data_ptr(), lddy, TYPE_CODES[dy.dtype], x.data_ptr(), ldx,
         TYPE_CODES[x.dtype], n, d, _at(weight), _at(mean), _at(rstd),
         _at(dres), lddres, _at(dx), d, _at(dw), _at(db), ws.data_ptr(),
-        nbytes, _raw_stream(dev.index)), "ezsp_layer_norm_backward")
+        nbytes,
+        _raw_stream(dev.index)), "ezsp_layer_norm_backward")
     return dx, dw, db
 
 
 def _weight(t, x, name, d_out=None):
     """A contiguous matrix [d_in, d_out] of x's type, on its device."""
-    _on_device(t, name, x)
+    if not isinstance(t, torch.Tensor) or t.get_device() != x.get_device():
+        _elsewhere(t, name, x)
     if t.dtype != x.dtype:
         raise TypeError(f"{name} must be {x.dtype}, got {t.dtype}")
     if t.dim() != 2 or t.shape[0] != x.shape[1] or \
@@ -685,7 +709,7 @@ def linear(x: torch.Tensor, w: torch.Tensor, bias=None, act: str = "none",
     z = torch.empty((n, d_out), dtype=ty, device=dev) if want_z else None
     nbytes = _dense_bytes("ezsp_linear_workspace_size", n, d_in, d_out)
     ws = _dense_ws(nbytes, dev)
-    _check(lib.ezsp_linear(
+    _check(_on(dev, lib.ezsp_linear)(
         x.data_ptr(), ldx, n, d_in, d_out, TYPE_CODES[ty], w.data_ptr(),
         _at(bias), code, _at(residual), ldr, y.data_ptr(), d_out,
         TYPE_CODES[out_dtype], _at(z), d_out, ws.data_ptr(), nbytes,
@@ -718,11 +742,11 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor,
     nbytes = _dense_bytes("ezsp_linear_backward_workspace_size", n, d_in,
                           d_out, TYPE_CODES[ty])
     ws = _dense_ws(nbytes, dev)
-    _check(lib.ezsp_linear_backward(
+    _check(_on(dev, lib.ezsp_linear_backward)(
         dy.data_ptr(), lddy, TYPE_CODES[dy.dtype], x.data_ptr(), ldx, n, d_in,
         d_out, TYPE_CODES[ty], w.data_ptr(), _at(z), ldz, code, _at(dx), d_in,
-        _at(dw), _at(db), ws.data_ptr(), nbytes, _raw_stream(dev.index)),
-        "ezsp_linear_backward")
+        _at(dw), _at(db), ws.data_ptr(), nbytes,
+        _raw_stream(dev.index)), "ezsp_linear_backward")
     return dx, dw, db
 
 
@@ -750,12 +774,11 @@ def gated_ff(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor,
         gate, up = torch.empty_like(h), torch.empty_like(h)
     nbytes = _dense_bytes("ezsp_gated_ff_workspace_size", n, d_in, d_out)
     ws = _dense_ws(nbytes, dev)
-    _check(lib.ezsp_gated_ff(
+    _check(_on(dev, lib.ezsp_gated_ff)(
         x.data_ptr(), ldx, n, d_in, d_out, TYPE_CODES[ty], w_gate.data_ptr(),
         _at(b_gate), w_up.data_ptr(), _at(b_up), code, h.data_ptr(), d_out,
         _at(gate), _at(up), d_out, ws.data_ptr(), nbytes,
-        _raw_stream(dev.index)),
-        "ezsp_gated_ff")
+        _raw_stream(dev.index)), "ezsp_gated_ff")
     return (h, gate, up) if want_saved else h
 
 
@@ -790,11 +813,10 @@ def gated_ff_backward(dh: torch.Tensor, x: torch.Tensor,
     nbytes = _dense_bytes("ezsp_gated_ff_backward_workspace_size", n, d_in,
                           d_out, TYPE_CODES[ty])
     ws = _dense_ws(nbytes, dev)
-    _check(lib.ezsp_gated_ff_backward(
+    _check(_on(dev, lib.ezsp_gated_ff_backward)(
         dh.data_ptr(), lddh, x.data_ptr(), ldx, n, d_in, d_out,
         TYPE_CODES[ty], w_gate.data_ptr(), w_up.data_ptr(), gate.data_ptr(),
         up.data_ptr(), lds, code, _at(dx), d_in, _at(dwg), _at(dwu),
         _at(dbg), _at(dbu), ws.data_ptr(), nbytes,
-        _raw_stream(dev.index)),
-        "ezsp_gated_ff_backward")
+        _raw_stream(dev.index)), "ezsp_gated_ff_backward")
     return dx, dwg, dwu, dbg, dbu

@@ -73,3 +73,27 @@ def test_two_devices_are_refused(op, other):
 def test_one_device_gets_as_far_as_its_results(op):
     with pytest.raises(AssertionError, match="allocated"):
         getattr(ezsp, op)(**arguments(OPERATORS[op], None))
+
+
+@pytest.mark.parametrize("current", [0, 1])
+def test_calls_run_on_their_tensors_device(monkeypatch, current):
+    # a default stream's handle names the current device's, whichever that is
+    state = dict(current=current, called=None)
+
+    class Current:
+        def __init__(self, device):
+            self.index = device.index
+
+        def __enter__(self):
+            self.before, state["current"] = state["current"], self.index
+
+        def __exit__(self, *error):
+            state["current"] = self.before
+
+    def entry(*args):
+        state["called"] = (state["current"], args)
+        return ezsp.OK
+    monkeypatch.setattr(torch.cuda, "device", Current)
+    monkeypatch.setattr(ezsp, "_current_device", lambda: state["current"])
+    assert ezsp._on(torch.device("cuda", 1), entry)(7, 8) == ezsp.OK
+    assert state == dict(current=current, called=(1, (7, 8)))
