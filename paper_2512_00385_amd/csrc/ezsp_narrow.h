@@ -392,6 +392,21 @@ inline size_t narrow_part_bytes(int64_t n, int64_t d_in, int64_t d_out,
   return (size_t)(parts * products * (d_in + 1) * d_out * 4);
 }
 
+// The most that any shape up to this one takes which the one-pass kernels
+// accept (fp32's are among bfloat16's), so that a workspace does not shrink
+// where they start or cease to serve.
+inline size_t narrow_room(int64_t n, int64_t d_in, int64_t d_out,
+                          int products) {
+  size_t most = 0;
+  for (int64_t k = 32; k <= 128; k *= 2)
+    for (int64_t m = 128; m <= 512; m *= 2)
+      if (narrow_fits(kVec, k, m, products))
+        most = std::max(most, narrow_part_bytes(n, std::min(d_in, k),
+                                                std::min(d_out, m),
+                                                products));
+  return most;
+}
+
 template <class Op, int NB, int DT, int COLS, int CH>
 void narrow_launch(const NarrowArgs<__bf16> &g, const Op &op, hipStream_t st) {
   static const int64_t slots = [] {

@@ -1,0 +1,34 @@
+"""Workspaces of the dense operators' backward passes: what the passes keep
+there and no more."""
+import os
+
+import pytest
+
+from paper_2512_00385_amd import ezsp
+
+pytestmark = pytest.mark.skipif(not os.path.exists(ezsp.LIB_PATH),
+                                reason="libezsp.so not built")
+
+SIZE = {0: 2, 1: 4}  # bytes of a bfloat16, of an fp32 value
+WIDTHS = [1, 7, 16, 31, 32, 33, 64, 65, 100, 128, 129, 200, 256, 257, 500, 512,
+          513, 4096]
+
+
+def padded(d):
+    return (d + 7) // 8 * 8
+
+
+@pytest.mark.parametrize("name,products", [("linear", 1), ("gated_ff", 2)])
+@pytest.mark.parametrize("ty", SIZE)
+@pytest.mark.parametrize("n", [65_536, 1_300_000])
+def test_backward(name, products, ty, n):
+    # dz, and the larger of a split product's parts (at most 128 MiB) and the
+    # one-pass kernel's: 1024 blocks' sums of at most 128 x 256 or 64 x 512
+    # values, in fp32, with a row for the bias
+    query = getattr(ezsp.load(), f"ezsp_{name}_backward_workspace_size")
+    parts = max(128 << 20, 1024 * 4 * 65 * 512)
+    for d_in in WIDTHS:
+        for d_out in WIDTHS:
+            dz = n * products * padded(d_out) * SIZE[ty]
+            assert query(n, d_in, d_out, ty) <= dz + parts + 4096, \
+                (d_in, d_out)
