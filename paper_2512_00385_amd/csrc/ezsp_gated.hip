@@ -236,7 +236,7 @@ void backward(const GatedArgs &a, hipStream_t st) {
 
 void gated_reserve(Arena &ar, int64_t n, int64_t d_in, int64_t d_out,
                    int32_t type, bool bwd, GatedArgs *a) {
-  a->part_bytes = gemm_part_bytes(d_in, n, d_out, 2);
+  a->part_bytes = gemm_fwd_bytes(n, d_in, d_out, 2);
   if (bwd) {
     // (sizes may not fall where the one-pass kernel starts to serve)
     const int64_t rows =

@@ -1150,5 +1150,17 @@ inline size_t gemm_part_bytes(int64_t k, int64_t m, int64_t n, int products) {
   return (size_t)std::min<double>(want, (double)((size_t)128 << 20)) + 256;
 }
 
+// The same for a forward product.  A sum of fewer than eight steps in either
+// type is not split, and for so few columns W alone is packed, into the half
+// of the space.
+inline size_t gemm_fwd_bytes(int64_t n, int64_t d_in, int64_t d_out,
+                             int products) {
+  constexpr int64_t kUnsplit = 7 * kLineBytes / (int64_t)sizeof(float);
+  const size_t parts = gemm_part_bytes(d_in, n, d_out, products);
+  if (d_in > kUnsplit || d_out * products >= kPackN) return parts;
+  const size_t w = (size_t)(products * d_in * pad_row(d_out)) * sizeof(float);
+  return std::min(parts, 2 * w + 1024);
+}
+
 }  // namespace
 }  // namespace ezsp

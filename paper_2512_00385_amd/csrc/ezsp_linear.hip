@@ -238,7 +238,7 @@ void backward(const LinearArgs &a, hipStream_t st) {
 
 void linear_reserve(Arena &ar, int64_t n, int64_t d_in, int64_t d_out,
                     int32_t type, bool bwd, LinearArgs *a) {
-  a->part_bytes = gemm_part_bytes(d_in, n, d_out, 1);
+  a->part_bytes = gemm_fwd_bytes(n, d_in, d_out, 1);
   if (bwd) {
     // the one-pass kernel needs its parts alone, but sizes may not fall where
     // it starts to serve

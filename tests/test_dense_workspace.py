@@ -1,5 +1,4 @@
-"""Workspaces of the dense operators' backward passes: what the passes keep
-there and no more."""
+"""Workspaces of the dense operators: what a call keeps there and no more."""
 import os
 
 import pytest
@@ -32,3 +31,15 @@ def test_backward(name, products, ty, n):
             dz = n * products * padded(d_out) * SIZE[ty]
             assert query(n, d_in, d_out, ty) <= dz + parts + 4096, \
                 (d_in, d_out)
+
+
+@pytest.mark.parametrize("name,products", [("linear", 1), ("gated_ff", 2)])
+def test_forward_of_few_columns(name, products):
+    # sums too short to be split, too few columns to pack x for: an aligned
+    # copy of the weights in half of it, at most
+    query = getattr(ezsp.load(), f"ezsp_{name}_workspace_size")
+    for n in (1000, 1_300_000, 2 ** 31 - 256):
+        for d_in in (1, 32, 224):
+            for d_out in (1, 64, 191 // products):
+                copy = products * d_in * padded(d_out) * 4
+                assert query(n, d_in, d_out) <= 2 * copy + 4096
