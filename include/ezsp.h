@@ -333,7 +333,7 @@ int ezsp_embed_mlp(const uint16_t *x, int64_t n, int32_t d_in, int32_t d_hid,
  * mean = sum(x) / d and rstd = 1 / sqrt(sum((x - mean)^2) / d + eps).
  *   x       n rows of d, type_x (in); d in 1..16384
  *   weight  d fp32 (in, nullable: 1); bias d fp32 (in, nullable: 0)
- *   eps     finite and >= 0
+ *   eps     >= 0, taken as fp32, where it must neither overflow nor vanish
  *   y       n rows of d, type_y (out); may be x when the types and row
  *           distances are the same
  *   mean, rstd  n fp32 each (out, nullable)

@@ -1,6 +1,7 @@
 // ezsp_api.hip -- the extern "C" entry points declared in include/ezsp.h:
 // argument validation on the host, workspace carving, and dispatch to the
 // kernel launchers.
+#include <float.h>
 #include <math.h>
 #include <string.h>
 
@@ -491,8 +492,11 @@ int ezsp_layer_norm(const void *x, int64_t ldx, int32_t type_x, int64_t n,
     return fail(EZSP_ERR_INVALID_ARG, "unknown element type");
   if (ldx < d || ldy < d)
     return fail(EZSP_ERR_INVALID_ARG, "row distances must be at least d");
-  if (!(eps >= 0.0) || !isfinite(eps))
-    return fail(EZSP_ERR_INVALID_ARG, "eps must be finite and >= 0");
+  // (the kernels hold it in fp32)
+  if (!(eps >= 0.0 && eps <= (double)FLT_MAX) ||
+      (eps > 0.0 && (float)eps == 0.0f))
+    return fail(EZSP_ERR_INVALID_ARG,
+                "eps must be >= 0 and neither overflow nor vanish in fp32");
   NormArgs a;
   memset(&a, 0, sizeof(a));
   a.x = x;
