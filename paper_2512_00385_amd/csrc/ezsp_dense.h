@@ -28,8 +28,6 @@ typedef u32x4_t u32x4_u4 __attribute__((aligned(4)));
 
 constexpr int kVec = 8;  // elements a lane takes at once
 
-__device__ __forceinline__ float bf16_to_f32(__bf16 v) { return (float)v; }
-
 // cnt elements (at most kVec) from p on as fp32, the rest 0
 __device__ __forceinline__ f32x8_t load8(const __bf16 *p, int cnt) {
   f32x8_t r = {0, 0, 0, 0, 0, 0, 0, 0};

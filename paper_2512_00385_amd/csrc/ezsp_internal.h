@@ -250,7 +250,7 @@ struct NormArgs {
   void *dx;               // nullable
   int64_t lddx;
   float *dw, *db;         // nullable
-  float *part;            // kNormParts * 2 * d
+  float *part;            // a row of 2 d a block: min(n, kNormParts) at most
 };
 constexpr int32_t kNormMaxD = 16384;
 constexpr int32_t kNormParts = 1024;
