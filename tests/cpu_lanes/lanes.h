@@ -85,6 +85,15 @@ V read_transposed(const void *p) {
   return v;
 }
 
+inline float exchange(float v, int by) {
+  Wave &w = wave();
+  memcpy(w.a[lane()], &v, 4);
+  wave_meets();
+  memcpy(&v, w.a[lane() ^ by], 4);
+  wave_meets();
+  return v;
+}
+
 inline uint32_t byte_permute(uint32_t hi, uint32_t lo, uint32_t select) {
   const uint64_t both = ((uint64_t)hi << 32) | lo;
   uint32_t r = 0;
@@ -159,7 +168,7 @@ int not_here(A...) {
 #define blockDim lanes::block_dim
 #define gridDim lanes::grid
 #define __syncthreads() lanes::block_meets()
-#define __shfl_xor(v, by, width) (v)
+#define __shfl_xor(v, by, width) lanes::exchange(v, by)
 #define __builtin_amdgcn_readfirstlane(v) (v)
 #define __builtin_amdgcn_wave_barrier() lanes::wave_meets()
 #define __builtin_amdgcn_sched_barrier(v) ((void)0)
