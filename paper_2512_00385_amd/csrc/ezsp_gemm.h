@@ -965,12 +965,27 @@ void pack_launch(const T *src, int64_t ld, int32_t rows, int32_t cols, T *dst,
 // D = A B through epi, whose parts lie in the part_bytes at epi.part.
 //
 // Operands at 16-byte alignment go past the registers into LDS, others
-// through them, at a third of the rate in products that fill the chip.  There
-// an unaligned operand is first packed into the same workspace, W whole and
-// the long one in chunks of rows; a copy of it costs 2 k e bytes a row, which
-// 2 n k multiplications at the higher rate repay from n = kPackN on.
+// through them, at half the rate in products that fill the chip.  There an
+// unaligned operand is first packed into the same workspace, W whole and the
+// long one in chunks of rows.  A copy of W costs next to nothing (20,000 x 512
+// -> 515: 33 us for 45; 300,000 x 256 -> 100: 73 for 91).  One of the long
+// operand costs 2 k e bytes a row, which 2 n k multiplications repay by n, the
+// columns of all B together.  Products of 1.2e11 operations, rows three values
+// longer than k, packed for unpacked, us:
+//                        n = 256        384          512          1024
+//   bf16, k = 64      1187 (1157)  1046 (1110)  1021 (1141)   947 (1075)
+//        512           419  (384)   382  (360)   308  (379)   253  (339)
+//   gated, k = 200     546  (568)   478  (522)   456  (550)   409  (485)
+//   x^T dz with dx, k = 200
+//                     1719 (1018)  1308  (926)   924  (905)   764  (905)
+//   gated, 200        1708 (1067)               857  (883)   753  (932)
+//   fp32 (a sixth of the operations), k = 512
+//                      261  (225)                222  (202)   195  (200)
+//   ... x^T dz with dx
+//                      848  (540)                440  (517)   422  (510)
+// Below kPackFlops the two differ by 2 us either way.
 constexpr double kPackFlops = 4e9;
-constexpr int32_t kPackN = 192;
+constexpr int32_t kPackN = 512;
 
 template <class T, bool AK, bool BK, int MODE, class Epi>
 void gemm(GemmArgs<T> g, Epi epi, size_t part_bytes, hipStream_t st) {
@@ -991,7 +1006,7 @@ void gemm(GemmArgs<T> g, Epi epi, size_t part_bytes, hipStream_t st) {
   size_t room = part_bytes & ~(size_t)255;
   const double flops = 2.0 * g.m * g.n * (double)g.k * kB;
   if ((!fast_a || !fast_b) && flops >= kPackFlops &&
-      (fast_a || (MODE != kSeq && (AK ? g.n : g.n + 64) * kB >= kPackN))) {
+      (fast_a || (MODE != kSeq && g.n * kB >= kPackN))) {
     const int64_t b_rows = BK ? g.n : g.k, b_cols = BK ? g.k : g.n;
     const size_t b_bytes =
         fast_b ? 0 : (size_t)(b_rows * pad_row(b_cols)) * e * kB;
