@@ -242,7 +242,8 @@ void gated_reserve(Arena &ar, int64_t n, int64_t d_in, int64_t d_out,
     const int64_t rows =
         narrow_serves(type, n, d_in, d_out, 2) ? kVec - 1 : n;
     a->part_bytes = std::max(
-        std::max(narrow_room(n, d_in, d_out, 2),
+        std::max(std::max(narrow_room(n, d_in, d_out, 2),
+                          gemm_pack_bytes(n, d_in, d_out, type, 2)),
                  (size_t)prep_parts(rows) * 2 * (size_t)d_out * 4),
         std::max(gemm_part_bytes(2 * d_out, rows, d_in, 1),
                  gemm_part_bytes(rows, d_in, d_out, 2)));

@@ -1165,6 +1165,20 @@ inline size_t gemm_part_bytes(int64_t k, int64_t m, int64_t n, int products) {
   return (size_t)std::min<double>(want, (double)((size_t)128 << 20)) + 256;
 }
 
+// Bytes that let a backward pass keep an aligned copy of x in half of them,
+// where that is worth making, at most 256 MiB a product (x then goes in
+// chunks).  Whether x is aligned is not known yet.
+inline size_t gemm_pack_bytes(int64_t n, int64_t d_in, int64_t d_out,
+                              int type, int products) {
+  const double flops = 2.0 * (double)n * (double)d_in * (double)d_out *
+                       products;
+  if (flops < kPackFlops || d_out * products < kPackN) return 0;
+  const double want = 2.0 * (double)(n + 256) * (double)pad_row(d_in) *
+                      (double)type_bytes(type);
+  return (size_t)std::min<double>(
+             want, (double)products * (double)((size_t)256 << 20)) + 512;
+}
+
 // The same for a forward product.  A sum of fewer than eight steps in either
 // type is not split, and for so few columns W alone is packed, into the half
 // of the space.

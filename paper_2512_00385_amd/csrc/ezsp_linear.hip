@@ -245,7 +245,8 @@ void linear_reserve(Arena &ar, int64_t n, int64_t d_in, int64_t d_out,
     const int64_t rows =
         narrow_serves(type, n, d_in, d_out, 1) ? kVec - 1 : n;
     a->part_bytes = std::max(
-        std::max(narrow_room(n, d_in, d_out, 1),
+        std::max(std::max(narrow_room(n, d_in, d_out, 1),
+                          gemm_pack_bytes(n, d_in, d_out, type, 1)),
                  (size_t)prep_parts(rows) * (size_t)d_out * 4),
         std::max(gemm_part_bytes(d_out, rows, d_in, 1),
                  gemm_part_bytes(rows, d_in, d_out, 1)));

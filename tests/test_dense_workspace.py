@@ -21,13 +21,17 @@ def padded(d):
 @pytest.mark.parametrize("ty", SIZE)
 @pytest.mark.parametrize("n", [65_536, 1_300_000])
 def test_backward(name, products, ty, n):
-    # dz, and the larger of a split product's parts (at most 128 MiB) and the
-    # one-pass kernel's: 1024 blocks' sums of at most 128 x 256 or 64 x 512
-    # values, in fp32, with a row for the bias
+    # dz, and the larger of a split product's parts (at most 128 MiB), the
+    # one-pass kernel's (1024 blocks' sums of at most 128 x 256 or 64 x 512
+    # values, in fp32, with a row for the bias) and, from 512 columns on,
+    # twice an aligned copy of x (at most 256 MiB a product)
     query = getattr(ezsp.load(), f"ezsp_{name}_backward_workspace_size")
-    parts = max(128 << 20, 1024 * 4 * 65 * 512)
     for d_in in WIDTHS:
         for d_out in WIDTHS:
+            parts = max(128 << 20, 1024 * 4 * 65 * 512)
+            if d_out * products >= 512:
+                copy = (n + 256) * padded(d_in) * SIZE[ty]
+                parts = max(parts, min(2 * copy, products << 28))
             dz = n * products * padded(d_out) * SIZE[ty]
             assert query(n, d_in, d_out, ty) <= dz + parts + 4096, \
                 (d_in, d_out)
