@@ -519,23 +519,21 @@ TYPE_CODES = {torch.bfloat16: 0, torch.float32: 1}
 ACT_CODES = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 
 
-def _elsewhere(t, name, like):
-    """Raises for a t that is not a tensor on like's device (any device
-    without)."""
+def _elsewhere(t, name, index):
+    """Raises for a t that is not a tensor on device `index` (None: any)."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a device tensor")
-    if like is not None:
-        raise ValueError(f"{name} must be on device {like.get_device()} as "
-                         f"x, is on {t.get_device()}")
+    raise ValueError(f"{name} must be on device {index} as x, is on "
+                     f"{t.get_device()}")
 
 
-def _rows(t, name, like=None, cols=None, dtype=None):
-    """A [n, d] device tensor whose rows are contiguous (columns of a wider
-    table stay as they are, other orders are copied) and the distance
-    between its rows; with `like` it has as many rows, on its device."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda or \
-            (like is not None and t.get_device() != like.get_device()):
-        _elsewhere(t, name, like)
+def _rows(t, name, index=None, shape=None, dtype=None):
+    """A [n, d] tensor on a device (`index`, if given) whose rows are
+    contiguous (columns of a wider table stay as they are, other orders are
+    copied) and the distance between its rows."""
+    if not isinstance(t, torch.Tensor) or \
+            (not t.is_cuda if index is None else t.get_device() != index):
+        _elsewhere(t, name, index)
     if dtype is not None and t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if t.dtype not in TYPE_CODES:
@@ -543,9 +541,9 @@ def _rows(t, name, like=None, cols=None, dtype=None):
     if t.dim() != 2:
         raise ValueError(f"{name} must have shape [n, d]")
     n, d = t.shape
-    if like is not None and (n != like.shape[0] or d != cols):
-        raise ValueError(f"{name} must have shape [{like.shape[0]}, {cols}], "
-                         f"got {list(t.shape)}")
+    if shape is not None and (n, d) != shape:
+        raise ValueError(f"{name} must have shape {list(shape)}, got "
+                         f"{list(t.shape)}")
     ld, one = t.stride()
     if (one != 1 and d > 1) or (ld < d and n > 1):
         t = t.contiguous()
@@ -553,13 +551,12 @@ def _rows(t, name, like=None, cols=None, dtype=None):
     return t, max(ld, d)
 
 
-def _vector(t, d, name, like):
-    """A contiguous fp32 vector of d values on like's device, or None."""
+def _vector(t, d, name, index):
+    """A contiguous fp32 vector of d values on device `index`, or None."""
     if t is None:
         return None
-    if not isinstance(t, torch.Tensor) or \
-            t.get_device() != like.get_device():
-        _elsewhere(t, name, like)
+    if not isinstance(t, torch.Tensor) or t.get_device() != index:
+        _elsewhere(t, name, index)
     if t.dtype != torch.float32:
         raise TypeError(f"{name} must be torch.float32, got {t.dtype}")
     if t.shape != (d,):
@@ -594,14 +591,14 @@ _current_device = getattr(torch._C, "_cuda_getDevice", None) or \
     torch.cuda.current_device
 
 
-def _on(device, fn):
-    """fn, called with the device made the current one: a default stream is
-    the current device's, whatever device it was asked of."""
-    if device.index == _current_device():
+def _on(index, fn):
+    """fn, called with device `index` made the current one: a default stream
+    is the current device's, whatever device it was asked of."""
+    if index == _current_device():
         return fn
 
     def call(*args):
-        with torch.cuda.device(device):
+        with torch.cuda.device(index):
             return fn(*args)
     return call
 
@@ -615,7 +612,9 @@ def layer_norm(x: torch.Tensor, weight=None, bias=None, eps: float = 1e-5,
     lib = load()
     x, ldx = _rows(x, "x")
     n, d = x.shape
-    weight, bias = _vector(weight, d, "weight", x), _vector(bias, d, "bias", x)
+    index = x.get_device()
+    weight = _vector(weight, d, "weight", index)
+    bias = _vector(bias, d, "bias", index)
     out_dtype = out_dtype or x.dtype
     if out_dtype not in TYPE_CODES:
         raise TypeError("out_dtype must be bfloat16 or float32")
@@ -624,11 +623,10 @@ def layer_norm(x: torch.Tensor, weight=None, bias=None, eps: float = 1e-5,
     if want_stats:
         mean = torch.empty(n, dtype=torch.float32, device=x.device)
         rstd = torch.empty(n, dtype=torch.float32, device=x.device)
-    _check(_on(x.device, lib.ezsp_layer_norm)(
+    _check(_on(index, lib.ezsp_layer_norm)(
         x.data_ptr(), ldx, TYPE_CODES[x.dtype], n, d, _at(weight), _at(bias),
         float(eps), y.data_ptr(), d, TYPE_CODES[out_dtype], _at(mean),
-        _at(rstd),
-        _raw_stream(x.device.index)), "ezsp_layer_norm")
+        _at(rstd), _raw_stream(index)), "ezsp_layer_norm")
     return (y, mean, rstd) if want_stats else y
 
 
@@ -642,12 +640,14 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor,
     lib = load()
     x, ldx = _rows(x, "x")
     n, d = x.shape
-    dy, lddy = _rows(dy, "dy", x, d)
-    mean, rstd = _vector(mean, n, "mean", x), _vector(rstd, n, "rstd", x)
-    weight = _vector(weight, d, "weight", x)
+    index = x.get_device()
+    dy, lddy = _rows(dy, "dy", index, (n, d))
+    mean = _vector(mean, n, "mean", index)
+    rstd = _vector(rstd, n, "rstd", index)
+    weight = _vector(weight, d, "weight", index)
     lddres = 0
     if dres is not None:
-        dres, lddres = _rows(dres, "dres", x, d, x.dtype)
+        dres, lddres = _rows(dres, "dres", index, (n, d), x.dtype)
     dev = x.device
     dx = torch.empty((n, d), dtype=x.dtype, device=dev) if want_dx else None
     dw = db = None
@@ -656,24 +656,24 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor,
         db = torch.empty(d, dtype=torch.float32, device=dev)
     nbytes = _dense_bytes("ezsp_layer_norm_backward_workspace_size", n, d)
     ws = _dense_ws(nbytes, dev)
-    _check(_on(dev, lib.ezsp_layer_norm_backward)(
+    _check(_on(index, lib.ezsp_layer_norm_backward)(
         dy.data_ptr(), lddy, TYPE_CODES[dy.dtype], x.data_ptr(), ldx,
         TYPE_CODES[x.dtype], n, d, _at(weight), _at(mean), _at(rstd),
         _at(dres), lddres, _at(dx), d, _at(dw), _at(db), ws.data_ptr(),
-        nbytes,
-        _raw_stream(dev.index)), "ezsp_layer_norm_backward")
+        nbytes, _raw_stream(index)), "ezsp_layer_norm_backward")
     return dx, dw, db
 
 
-def _weight(t, x, name, d_out=None):
-    """A contiguous matrix [d_in, d_out] of x's type, on its device."""
-    if not isinstance(t, torch.Tensor) or t.get_device() != x.get_device():
-        _elsewhere(t, name, x)
-    if t.dtype != x.dtype:
-        raise TypeError(f"{name} must be {x.dtype}, got {t.dtype}")
-    if t.dim() != 2 or t.shape[0] != x.shape[1] or \
+def _weight(t, d_in, dtype, name, index, d_out=None):
+    """A contiguous matrix [d_in, d_out] of the given type on device
+    `index`."""
+    if not isinstance(t, torch.Tensor) or t.get_device() != index:
+        _elsewhere(t, name, index)
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.dim() != 2 or t.shape[0] != d_in or \
             (d_out is not None and t.shape[1] != d_out):
-        raise ValueError(f"{name} must have shape [{x.shape[1]}, "
+        raise ValueError(f"{name} must have shape [{d_in}, "
                          f"{'d_out' if d_out is None else d_out}]")
     return t.contiguous()
 
@@ -694,26 +694,27 @@ def linear(x: torch.Tensor, w: torch.Tensor, bias=None, act: str = "none",
     lib = load()
     x, ldx = _rows(x, "x")
     n, d_in = x.shape
-    ty, dev = x.dtype, x.device
-    w = _weight(w, x, "w")
+    ty, dev, index = x.dtype, x.device, x.get_device()
+    w = _weight(w, d_in, ty, "w", index)
     d_out = w.shape[1]
     code = _act(act)
-    bias = _vector(bias, d_out, "bias", x)
+    bias = _vector(bias, d_out, "bias", index)
     out_dtype = out_dtype or ty
     if out_dtype not in (ty, torch.float32):
         raise TypeError("out_dtype must be x's type or float32")
     ldr = 0
     if residual is not None:
-        residual, ldr = _rows(residual, "residual", x, d_out, out_dtype)
+        residual, ldr = _rows(residual, "residual", index, (n, d_out),
+                              out_dtype)
     y = torch.empty((n, d_out), dtype=out_dtype, device=dev)
     z = torch.empty((n, d_out), dtype=ty, device=dev) if want_z else None
     nbytes = _dense_bytes("ezsp_linear_workspace_size", n, d_in, d_out)
     ws = _dense_ws(nbytes, dev)
-    _check(_on(dev, lib.ezsp_linear)(
+    _check(_on(index, lib.ezsp_linear)(
         x.data_ptr(), ldx, n, d_in, d_out, TYPE_CODES[ty], w.data_ptr(),
         _at(bias), code, _at(residual), ldr, y.data_ptr(), d_out,
         TYPE_CODES[out_dtype], _at(z), d_out, ws.data_ptr(), nbytes,
-        _raw_stream(dev.index)), "ezsp_linear")
+        _raw_stream(index)), "ezsp_linear")
     return (y, z) if want_z else y
 
 
@@ -727,14 +728,14 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor,
     lib = load()
     x, ldx = _rows(x, "x")
     n, d_in = x.shape
-    ty, dev = x.dtype, x.device
-    w = _weight(w, x, "w")
+    ty, dev, index = x.dtype, x.device, x.get_device()
+    w = _weight(w, d_in, ty, "w", index)
     d_out = w.shape[1]
     code = _act(act)
-    dy, lddy = _rows(dy, "dy", x, d_out)
+    dy, lddy = _rows(dy, "dy", index, (n, d_out))
     ldz = 0
     if z is not None:
-        z, ldz = _rows(z, "z", x, d_out, ty)
+        z, ldz = _rows(z, "z", index, (n, d_out), ty)
     dx = torch.empty((n, d_in), dtype=ty, device=dev) if want_dx else None
     dw = torch.empty((d_in, d_out), dtype=ty, device=dev) if want_dw else None
     db = torch.empty(d_out, dtype=torch.float32, device=dev) \
@@ -742,11 +743,11 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor,
     nbytes = _dense_bytes("ezsp_linear_backward_workspace_size", n, d_in,
                           d_out, TYPE_CODES[ty])
     ws = _dense_ws(nbytes, dev)
-    _check(_on(dev, lib.ezsp_linear_backward)(
+    _check(_on(index, lib.ezsp_linear_backward)(
         dy.data_ptr(), lddy, TYPE_CODES[dy.dtype], x.data_ptr(), ldx, n, d_in,
         d_out, TYPE_CODES[ty], w.data_ptr(), _at(z), ldz, code, _at(dx), d_in,
         _at(dw), _at(db), ws.data_ptr(), nbytes,
-        _raw_stream(dev.index)), "ezsp_linear_backward")
+        _raw_stream(index)), "ezsp_linear_backward")
     return dx, dw, db
 
 
@@ -761,24 +762,24 @@ def gated_ff(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor,
     lib = load()
     x, ldx = _rows(x, "x")
     n, d_in = x.shape
-    ty, dev = x.dtype, x.device
-    w_gate = _weight(w_gate, x, "w_gate")
+    ty, dev, index = x.dtype, x.device, x.get_device()
+    w_gate = _weight(w_gate, d_in, ty, "w_gate", index)
     d_out = w_gate.shape[1]
-    w_up = _weight(w_up, x, "w_up", d_out)
+    w_up = _weight(w_up, d_in, ty, "w_up", index, d_out)
     code = _act(act)
-    b_gate = _vector(b_gate, d_out, "b_gate", x)
-    b_up = _vector(b_up, d_out, "b_up", x)
+    b_gate = _vector(b_gate, d_out, "b_gate", index)
+    b_up = _vector(b_up, d_out, "b_up", index)
     h = torch.empty((n, d_out), dtype=ty, device=dev)
     gate = up = None
     if want_saved:
         gate, up = torch.empty_like(h), torch.empty_like(h)
     nbytes = _dense_bytes("ezsp_gated_ff_workspace_size", n, d_in, d_out)
     ws = _dense_ws(nbytes, dev)
-    _check(_on(dev, lib.ezsp_gated_ff)(
+    _check(_on(index, lib.ezsp_gated_ff)(
         x.data_ptr(), ldx, n, d_in, d_out, TYPE_CODES[ty], w_gate.data_ptr(),
         _at(b_gate), w_up.data_ptr(), _at(b_up), code, h.data_ptr(), d_out,
         _at(gate), _at(up), d_out, ws.data_ptr(), nbytes,
-        _raw_stream(dev.index)), "ezsp_gated_ff")
+        _raw_stream(index)), "ezsp_gated_ff")
     return (h, gate, up) if want_saved else h
 
 
@@ -793,14 +794,14 @@ def gated_ff_backward(dh: torch.Tensor, x: torch.Tensor,
     lib = load()
     x, ldx = _rows(x, "x")
     n, d_in = x.shape
-    ty, dev = x.dtype, x.device
-    w_gate = _weight(w_gate, x, "w_gate")
+    ty, dev, index = x.dtype, x.device, x.get_device()
+    w_gate = _weight(w_gate, d_in, ty, "w_gate", index)
     d_out = w_gate.shape[1]
-    w_up = _weight(w_up, x, "w_up", d_out)
+    w_up = _weight(w_up, d_in, ty, "w_up", index, d_out)
     code = _act(act)
-    dh, lddh = _rows(dh, "dh", x, d_out, ty)
-    gate, lds = _rows(gate, "gate", x, d_out, ty)
-    up, lds_up = _rows(up, "up", x, d_out, ty)
+    dh, lddh = _rows(dh, "dh", index, (n, d_out), ty)
+    gate, lds = _rows(gate, "gate", index, (n, d_out), ty)
+    up, lds_up = _rows(up, "up", index, (n, d_out), ty)
     if lds != lds_up:
         gate, up, lds = gate.contiguous(), up.contiguous(), d_out
     dx = torch.empty((n, d_in), dtype=ty, device=dev) if want_dx else None
@@ -813,10 +814,10 @@ def gated_ff_backward(dh: torch.Tensor, x: torch.Tensor,
     nbytes = _dense_bytes("ezsp_gated_ff_backward_workspace_size", n, d_in,
                           d_out, TYPE_CODES[ty])
     ws = _dense_ws(nbytes, dev)
-    _check(_on(dev, lib.ezsp_gated_ff_backward)(
+    _check(_on(index, lib.ezsp_gated_ff_backward)(
         dh.data_ptr(), lddh, x.data_ptr(), ldx, n, d_in, d_out,
         TYPE_CODES[ty], w_gate.data_ptr(), w_up.data_ptr(), gate.data_ptr(),
         up.data_ptr(), lds, code, _at(dx), d_in, _at(dwg), _at(dwu),
         _at(dbg), _at(dbu), ws.data_ptr(), nbytes,
-        _raw_stream(dev.index)), "ezsp_gated_ff_backward")
+        _raw_stream(index)), "ezsp_gated_ff_backward")
     return dx, dwg, dwu, dbg, dbu

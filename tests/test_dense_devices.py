@@ -76,13 +76,14 @@ def test_one_device_gets_as_far_as_its_results(op):
 
 
 @pytest.mark.parametrize("current", [0, 1])
-def test_calls_run_on_their_tensors_device(monkeypatch, current):
+@pytest.mark.parametrize("op", OPERATORS)
+def test_calls_run_on_their_tensors_device(monkeypatch, op, current):
     # a default stream's handle names the current device's, whichever that is
     state = dict(current=current, called=None)
 
     class Current:
         def __init__(self, device):
-            self.index = device.index
+            self.index = device
 
         def __enter__(self):
             self.before, state["current"] = state["current"], self.index
@@ -90,10 +91,20 @@ def test_calls_run_on_their_tensors_device(monkeypatch, current):
         def __exit__(self, *error):
             state["current"] = self.before
 
-    def entry(*args):
-        state["called"] = (state["current"], args)
-        return ezsp.OK
-    monkeypatch.setattr(torch.cuda, "device", Current)
+    class Library:
+        def __getattr__(self, name):
+            def entry(*args):
+                state["called"] = (name, state["current"], args[-1])
+                return ezsp.OK
+            return entry
+    monkeypatch.setattr(ezsp, "load", Library)
+    monkeypatch.setattr(ezsp, "_dense_bytes", lambda *sizes: 512)
+    monkeypatch.setattr(ezsp, "_raw_stream", lambda index: 100 + index)
     monkeypatch.setattr(ezsp, "_current_device", lambda: state["current"])
-    assert ezsp._on(torch.device("cuda", 1), entry)(7, 8) == ezsp.OK
-    assert state == dict(current=current, called=(1, (7, 8)))
+    monkeypatch.setattr(torch.cuda, "device", Current)
+    monkeypatch.setattr(torch, "empty", lambda size, dtype, device:
+                        torch.zeros(size, dtype=dtype))
+    args = {name: on(ClaimsOther, *shape, dtype=dtype)
+            for name, (shape, dtype) in OPERATORS[op].items()}
+    getattr(ezsp, op)(**args)
+    assert state == dict(current=current, called=("ezsp_" + op, 1, 101))
