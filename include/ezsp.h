@@ -24,7 +24,8 @@
  *   - ezsp_knn, ezsp_component_stats, ezsp_embed_mlp and the dense operators
  *     (ezsp_layer_norm and after) are stream-asynchronous: they validate
  *     their arguments, enqueue their kernels and return; their outputs are
- *     ready once `stream` reaches that point, and their workspace must stay allocated until then.
+ *     ready once `stream` reaches that point, and their workspace must stay
+ *     allocated until then.
  *     Errors the device detects (a non-finite coordinate, a label out of
  *     range) are kept in the call's workspace and reported by
  *     ezsp_sync_status.  The entry points that return host values
@@ -480,9 +481,10 @@ const char *ezsp_last_error(void);
  * the launches of each stage ("knn_query", "morton_sort", "graph_build",
  * "select", "union", "stats", "contract", "compose", "tail", "link",
  * "grid_subsample", "edge_loss", "purity", "embed_mlp", "layer_norm",
- * "linear", "gated_ff").  Off by default; a diagnostic for benchmarks.  ezsp_profile_enable(1) clears the totals and
- * starts recording, ezsp_profile_enable(0) stops.  ezsp_profile_read gives
- * the number of recorded launches of `stage`, their summed duration in
+ * "linear", "gated_ff").  Off by default; a diagnostic for benchmarks.
+ * ezsp_profile_enable(1) clears the totals and starts recording,
+ * ezsp_profile_enable(0) stops.  ezsp_profile_read gives the number of
+ * recorded launches of `stage`, their summed duration in
  * milliseconds and the summed algorithmic bytes the stage has to move (its
  * input and output arrays, each counted once; host pointers, each
  * nullable); it returns -1, with zeros, for a stage never recorded.

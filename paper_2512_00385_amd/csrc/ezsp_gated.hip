@@ -4,7 +4,8 @@
 // activation and the product happen on its accumulators), and its gradients
 //   dg = dh u act'(g),  du = dh act(g),
 //   dx = dg Wg^T + du Wu^T,  dWg = x^T dg,  dWu = x^T du,  db = row sums.
-// dg and du are formed once, side by side in one table; dx sums over both in
+// dg and du are formed once, side by side in one table (in bfloat16 for
+// bfloat16 inputs, the matrix cores' operands); dx sums over both in
 // one product of twice the length, and both weights' gradients come from one
 // pass over x.  Few columns take the one-pass kernel instead.
 #include "ezsp_few.h"

@@ -129,11 +129,12 @@ __global__ __launch_bounds__(kNFwdNT, 2) void k_narrow_fwd(GemmArgs<T> g,
 // the tiles of ezsp_gemm.h, us (floor at 4.9 TB/s); s: with residual or
 // pre-activations saved
 //                    linear          linear, s        gated       gated, s
-//   bf16   6 ->   6  24 for 40 ( 4)  40 for 51 ( 8)  27 for 69   33 for 78
-//         32 ->  32  22 for 28 (21)  34 for 35 (42)  25 for 41   34 for 45
-//         32 ->  64  33 for 50 (31) 113 for 108 (73) 37 for 59  109 for 90
-//   fp32   6 ->   6  28 for 47 ( 8)  42 for 56 (16)  38 for 79   48 for 87
-//          6 ->  32  29 for 45 (25)  79 for 73 (67)  35 for 73  104 for 99
+//   bf16   6 ->   6  22 for 42 ( 4)  36 for 53 ( 8)  26 for 73   31 for 82
+//          6 ->  32  21 for 39 (12)  29 for 44 (33)  23 for 58   28 for 60
+//         32 ->  32  22 for 27 (21)  33 for 34 (42)  24 for 40   33 for 43
+//         32 ->  64  32 for 46 (31) 114 for 112 (73) 37 for 60  104 for 95
+//   fp32   6 ->   6  27 for 49 ( 8)  40 for 58 (16)  38 for 85   47 for 93
+//          6 ->  32  28 for 48 (25)  83 for 80 (67)  35 for 79  106 for 126
 // The tiles store whole lines where a lane's rows here are half of one apart,
 // which costs once the results leave the caches: with 256 bytes the saved
 // forms lose more (bf16 32 -> 128, gated: 211 for 135) than the others gain

@@ -514,6 +514,9 @@ def embed_mlp(x_bits: torch.Tensor, w1, b1, w2, b2, w3, b3) -> torch.Tensor:
 
 
 # ---- dense operators of a trainable embedding network ---------------------
+#
+# Results lie outside torch's automatic differentiation, whether or not an
+# input requires gradients: the gradients are those of the *_backward calls.
 
 TYPE_CODES = {torch.bfloat16: 0, torch.float32: 1}
 ACT_CODES = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
@@ -608,7 +611,8 @@ def layer_norm(x: torch.Tensor, weight=None, bias=None, eps: float = 1e-5,
     """Layer norm over each row of x [n, d] (ezsp_layer_norm), bfloat16 or
     fp32, weight and bias [d] fp32 or None; y has out_dtype (x's by
     default).  Returns y, or with want_stats (y, mean [n], rstd [n]) for
-    layer_norm_backward.  Computed in stream order."""
+    layer_norm_backward, which is where gradients come from: torch's own
+    differentiation stops here.  Computed in stream order."""
     lib = load()
     x, ldx = _rows(x, "x")
     n, d = x.shape
@@ -690,7 +694,8 @@ def linear(x: torch.Tensor, w: torch.Tensor, bias=None, act: str = "none",
     w [d_in, d_out] bfloat16 or fp32, bias [d_out] fp32, residual [n, d_out]
     of y's type, which is out_dtype (x's by default, or fp32).  act: none,
     relu, gelu, silu.  Returns y, or with want_z (y, x w + bias) for
-    linear_backward.  Computed in stream order."""
+    linear_backward, which is where gradients come from: torch's own
+    differentiation stops here.  Computed in stream order."""
     lib = load()
     x, ldx = _rows(x, "x")
     n, d_in = x.shape
@@ -724,7 +729,7 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor,
     """Gradients of linear (ezsp_linear_backward): (dx, dw of x's type,
     dbias fp32), each None where it is not wanted.  dy [n, d_out] has x's
     type or fp32; z is linear's second result (not needed without an
-    activation)."""
+    activation).  With bfloat16, dx and dw take dy act'(z) rounded to it."""
     lib = load()
     x, ldx = _rows(x, "x")
     n, d_in = x.shape
@@ -757,8 +762,8 @@ def gated_ff(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor,
     """h = act(x w_gate + b_gate) * (x w_up + b_up) in one kernel
     (ezsp_gated_ff): x [n, d_in], weights [d_in, d_out], bfloat16 or fp32,
     biases [d_out] fp32 or None.  Returns h, or with want_saved (h, gate,
-    up), the two sums that gated_ff_backward reads.  Computed in stream
-    order."""
+    up), the two sums that gated_ff_backward reads; gradients come from it,
+    torch's own differentiation stops here.  Computed in stream order."""
     lib = load()
     x, ldx = _rows(x, "x")
     n, d_in = x.shape
@@ -790,7 +795,8 @@ def gated_ff_backward(dh: torch.Tensor, x: torch.Tensor,
                       want_dw: bool = True, want_db: bool = True):
     """Gradients of gated_ff (ezsp_gated_ff_backward): (dx, dw_gate, dw_up of
     x's type, db_gate, db_up fp32), None where not wanted; gate and up are
-    gated_ff's saved sums."""
+    gated_ff's saved sums.  With bfloat16, dx, dw_gate and dw_up take the
+    gradients of gate and up rounded to it."""
     lib = load()
     x, ldx = _rows(x, "x")
     n, d_in = x.shape
