@@ -572,8 +572,8 @@ def _at(t):
 
 
 # The calls below may take less time on the GPU than their arguments on the
-# host, so their sizes are queried once each and the stream is read without
-# torch's Stream object.
+# host, so their sizes are queried once each, the device and the stream are
+# read without torch's objects, and what follows a call is in line.
 @functools.lru_cache(maxsize=4096)
 def _dense_bytes(name: str, *sizes) -> int:
     nbytes = getattr(load(), name)(*sizes)
@@ -597,9 +597,6 @@ _current_device = getattr(torch._C, "_cuda_getDevice", None) or \
 def _on(index, fn):
     """fn, called with device `index` made the current one: a default stream
     is the current device's, whatever device it was asked of."""
-    if index == _current_device():
-        return fn
-
     def call(*args):
         with torch.cuda.device(index):
             return fn(*args)
@@ -627,10 +624,14 @@ def layer_norm(x: torch.Tensor, weight=None, bias=None, eps: float = 1e-5,
     if want_stats:
         mean = torch.empty(n, dtype=torch.float32, device=x.device)
         rstd = torch.empty(n, dtype=torch.float32, device=x.device)
-    _check(_on(index, lib.ezsp_layer_norm)(
+    fn = lib.ezsp_layer_norm if index == _current_device() else \
+        _on(index, lib.ezsp_layer_norm)
+    rc = fn(
         x.data_ptr(), ldx, TYPE_CODES[x.dtype], n, d, _at(weight), _at(bias),
         float(eps), y.data_ptr(), d, TYPE_CODES[out_dtype], _at(mean),
-        _at(rstd), _raw_stream(index)), "ezsp_layer_norm")
+        _at(rstd), _raw_stream(index))
+    if rc != OK:
+        _check(rc, "ezsp_layer_norm")
     return (y, mean, rstd) if want_stats else y
 
 
@@ -660,11 +661,15 @@ def layer_norm_backward(dy: torch.Tensor, x: torch.Tensor,
         db = torch.empty(d, dtype=torch.float32, device=dev)
     nbytes = _dense_bytes("ezsp_layer_norm_backward_workspace_size", n, d)
     ws = _dense_ws(nbytes, dev)
-    _check(_on(index, lib.ezsp_layer_norm_backward)(
+    fn = lib.ezsp_layer_norm_backward if index == _current_device() else \
+        _on(index, lib.ezsp_layer_norm_backward)
+    rc = fn(
         dy.data_ptr(), lddy, TYPE_CODES[dy.dtype], x.data_ptr(), ldx,
         TYPE_CODES[x.dtype], n, d, _at(weight), _at(mean), _at(rstd),
         _at(dres), lddres, _at(dx), d, _at(dw), _at(db), ws.data_ptr(),
-        nbytes, _raw_stream(index)), "ezsp_layer_norm_backward")
+        nbytes, _raw_stream(index))
+    if rc != OK:
+        _check(rc, "ezsp_layer_norm_backward")
     return dx, dw, db
 
 
@@ -715,11 +720,15 @@ def linear(x: torch.Tensor, w: torch.Tensor, bias=None, act: str = "none",
     z = torch.empty((n, d_out), dtype=ty, device=dev) if want_z else None
     nbytes = _dense_bytes("ezsp_linear_workspace_size", n, d_in, d_out)
     ws = _dense_ws(nbytes, dev)
-    _check(_on(index, lib.ezsp_linear)(
+    fn = lib.ezsp_linear if index == _current_device() else \
+        _on(index, lib.ezsp_linear)
+    rc = fn(
         x.data_ptr(), ldx, n, d_in, d_out, TYPE_CODES[ty], w.data_ptr(),
         _at(bias), code, _at(residual), ldr, y.data_ptr(), d_out,
         TYPE_CODES[out_dtype], _at(z), d_out, ws.data_ptr(), nbytes,
-        _raw_stream(index)), "ezsp_linear")
+        _raw_stream(index))
+    if rc != OK:
+        _check(rc, "ezsp_linear")
     return (y, z) if want_z else y
 
 
@@ -748,11 +757,15 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor,
     nbytes = _dense_bytes("ezsp_linear_backward_workspace_size", n, d_in,
                           d_out, TYPE_CODES[ty])
     ws = _dense_ws(nbytes, dev)
-    _check(_on(index, lib.ezsp_linear_backward)(
+    fn = lib.ezsp_linear_backward if index == _current_device() else \
+        _on(index, lib.ezsp_linear_backward)
+    rc = fn(
         dy.data_ptr(), lddy, TYPE_CODES[dy.dtype], x.data_ptr(), ldx, n, d_in,
         d_out, TYPE_CODES[ty], w.data_ptr(), _at(z), ldz, code, _at(dx), d_in,
         _at(dw), _at(db), ws.data_ptr(), nbytes,
-        _raw_stream(index)), "ezsp_linear_backward")
+        _raw_stream(index))
+    if rc != OK:
+        _check(rc, "ezsp_linear_backward")
     return dx, dw, db
 
 
@@ -780,11 +793,15 @@ def gated_ff(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor,
         gate, up = torch.empty_like(h), torch.empty_like(h)
     nbytes = _dense_bytes("ezsp_gated_ff_workspace_size", n, d_in, d_out)
     ws = _dense_ws(nbytes, dev)
-    _check(_on(index, lib.ezsp_gated_ff)(
+    fn = lib.ezsp_gated_ff if index == _current_device() else \
+        _on(index, lib.ezsp_gated_ff)
+    rc = fn(
         x.data_ptr(), ldx, n, d_in, d_out, TYPE_CODES[ty], w_gate.data_ptr(),
         _at(b_gate), w_up.data_ptr(), _at(b_up), code, h.data_ptr(), d_out,
         _at(gate), _at(up), d_out, ws.data_ptr(), nbytes,
-        _raw_stream(index)), "ezsp_gated_ff")
+        _raw_stream(index))
+    if rc != OK:
+        _check(rc, "ezsp_gated_ff")
     return (h, gate, up) if want_saved else h
 
 
@@ -820,10 +837,14 @@ def gated_ff_backward(dh: torch.Tensor, x: torch.Tensor,
     nbytes = _dense_bytes("ezsp_gated_ff_backward_workspace_size", n, d_in,
                           d_out, TYPE_CODES[ty])
     ws = _dense_ws(nbytes, dev)
-    _check(_on(index, lib.ezsp_gated_ff_backward)(
+    fn = lib.ezsp_gated_ff_backward if index == _current_device() else \
+        _on(index, lib.ezsp_gated_ff_backward)
+    rc = fn(
         dh.data_ptr(), lddh, x.data_ptr(), ldx, n, d_in, d_out,
         TYPE_CODES[ty], w_gate.data_ptr(), w_up.data_ptr(), gate.data_ptr(),
         up.data_ptr(), lds, code, _at(dx), d_in, _at(dwg), _at(dwu),
         _at(dbg), _at(dbu), ws.data_ptr(), nbytes,
-        _raw_stream(index)), "ezsp_gated_ff_backward")
+        _raw_stream(index))
+    if rc != OK:
+        _check(rc, "ezsp_gated_ff_backward")
     return dx, dwg, dwu, dbg, dbu
