@@ -974,6 +974,7 @@ void pack_launch(const T *src, int64_t ld, int32_t rows, int32_t cols, T *dst,
 // longer than k, packed for unpacked, us:
 //                        n = 256        384          512          1024
 //   bf16, k = 64      1187 (1157)  1046 (1110)  1021 (1141)   947 (1075)
+//        200           662  (645)   550  (597)   578  (628)   500  (555)
 //        512           419  (384)   382  (360)   308  (379)   253  (339)
 //   gated, k = 200     546  (568)   478  (522)   456  (550)   409  (485)
 //   x^T dz with dx, k = 200
@@ -983,10 +984,15 @@ void pack_launch(const T *src, int64_t ld, int32_t rows, int32_t cols, T *dst,
 //                      261  (225)                222  (202)   195  (200)
 //   ... x^T dz with dx
 //                      848  (540)                440  (517)   422  (510)
+// So 512 columns, and forward 384 where k is short.
 // Below kPackFlops the two differ by up to 6 us either way (4000 x 515 -> 515,
 // bf16: 24 us packed, 25 as it lies, backward 48 and 53; fp32 57 and 52).
 constexpr double kPackFlops = 4e9;
 constexpr int32_t kPackN = 512;
+constexpr int32_t kPackShortN = 384, kPackShortK = 256;
+inline bool pack_pays(bool forward, int64_t k, int64_t n) {
+  return n >= (forward && k <= kPackShortK ? kPackShortN : kPackN);
+}
 
 template <class T, bool AK, bool BK, int MODE, class Epi>
 void gemm(GemmArgs<T> g, Epi epi, size_t part_bytes, hipStream_t st) {
@@ -1007,7 +1013,7 @@ void gemm(GemmArgs<T> g, Epi epi, size_t part_bytes, hipStream_t st) {
   size_t room = part_bytes & ~(size_t)255;
   const double flops = 2.0 * g.m * g.n * (double)g.k * kB;
   if ((!fast_a || !fast_b) && flops >= kPackFlops &&
-      (fast_a || (MODE != kSeq && g.n * kB >= kPackN))) {
+      (fast_a || (MODE != kSeq && pack_pays(AK, g.k, (int64_t)g.n * kB)))) {
     const int64_t b_rows = BK ? g.n : g.k, b_cols = BK ? g.k : g.n;
     const size_t b_bytes =
         fast_b ? 0 : (size_t)(b_rows * pad_row(b_cols)) * e * kB;
@@ -1173,7 +1179,7 @@ inline size_t gemm_pack_bytes(int64_t n, int64_t d_in, int64_t d_out,
                               int type, int products) {
   const double flops = 2.0 * (double)n * (double)d_in * (double)d_out *
                        products;
-  if (flops < kPackFlops || d_out * products < kPackN) return 0;
+  if (flops < kPackFlops || !pack_pays(false, n, d_out * products)) return 0;
   const double want = 2.0 * (double)(n + 256) * (double)pad_row(d_in) *
                       (double)type_bytes(type);
   return (size_t)std::min<double>(
@@ -1187,7 +1193,8 @@ inline size_t gemm_fwd_bytes(int64_t n, int64_t d_in, int64_t d_out,
                              int products) {
   constexpr int64_t kUnsplit = 7 * kLineBytes / (int64_t)sizeof(float);
   const size_t parts = gemm_part_bytes(d_in, n, d_out, products);
-  if (d_in > kUnsplit || d_out * products >= kPackN) return parts;
+  if (d_in > kUnsplit || pack_pays(true, d_in, d_out * products))
+    return parts;
   const size_t w = (size_t)(products * d_in * pad_row(d_out)) * sizeof(float);
   return std::min(parts, 2 * w + 1024);
 }

@@ -1,5 +1,5 @@
-"""Unaligned products of 512 columns or more: the long operand is packed, in
-chunks where its copy is larger than the workspace allows, and their results
+"""Unaligned products of 384 or 512 columns or more: the long operand is packed,
+in chunks where its copy is larger than the workspace allows, and their results
 and sums put together.  On integers, for equality with 64 bits."""
 import pytest
 import torch
@@ -20,7 +20,8 @@ def gpu():
 
 
 # one chunk; several, the last of them short
-SIZES = [(20_011, 130, 515), (600_000, 130, 515), (330_007, 515, 512)]
+SIZES = [(20_011, 130, 515), (600_000, 130, 515), (330_007, 515, 512),
+         (200_003, 201, 390), (400_003, 201, 384)]
 
 
 @pytest.mark.parametrize("ty", [BF, F32])
@@ -44,7 +45,7 @@ def test_linear(n, k, m, ty):
 
 @pytest.mark.parametrize("ty", [BF, F32])
 @pytest.mark.parametrize("n,k,m", [(20_011, 130, 260), (500_000, 131, 260),
-                                   (330_007, 515, 256)])
+                                   (330_007, 515, 256), (200_003, 201, 195)])
 def test_gated(n, k, m, ty):
     g = generator(n + k + m)
     x, dh, gate, up = (integers(g, (n, d), 2, ty) for d in (k, m, m, m))
