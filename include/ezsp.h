@@ -583,7 +583,9 @@ size_t ezsp_cross_attention_workspace_size(int64_t nq, int64_t nk,
  *           kv_heads, at most 1024; d_head in 1..128; nq * heads < 2^31 and
  *           nk * kv_heads < 2^31
  *   q_offsets, k_offsets  n_clouds + 1 int32 (in, both or neither; NULL:
- *           one cloud; n_clouds at most 2^24): rows [offsets[c],
+ *           one cloud; n_clouds at most 2^24, and (n_clouds + 2) kv_heads
+ *           below 2^25 less the greater of nq heads / 64 and nk kv_heads /
+ *           64): rows [offsets[c],
  *           offsets[c + 1]) of q and of k and v are cloud c, any of them
  *           empty.  They must not decrease and must lie in [0, nq] and
  *           [0, nk]; others leave results unspecified, and nothing outside

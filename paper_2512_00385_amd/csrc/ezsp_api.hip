@@ -94,7 +94,8 @@ int check_attention(int64_t nq, int64_t nk, int32_t heads, int32_t kv_heads,
                 "q_offsets and k_offsets belong together");
   if (q_offsets && (n_clouds < 1 || n_clouds > 1 << 24))
     return fail(EZSP_ERR_INVALID_ARG, "n_clouds must be in 1..2^24");
-  // (a block takes at least 64 columns of a cloud, a launch 2^31 blocks)
+  // (a block takes at least 64 columns of a cloud, in up to 64 parts; a launch
+  // of attention 2^31 blocks, in rows)
   if (q_offsets && ((nq * (heads / kv_heads) / 64 + n_clouds + 2) * kv_heads >=
                         kMaxN / 64 ||
                     (nk / 64 + n_clouds + 2) * kv_heads >= kMaxN / 64))

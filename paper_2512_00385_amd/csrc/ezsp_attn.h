@@ -495,6 +495,18 @@ __device__ __forceinline__ Column q_column(const Attn &a, const Cloud &cl,
 
 constexpr int kFewUnits = 32;  // in order: some XCDs would have none
 
+// A launch has fewer than 2^32 threads along x, so that more than kGridRow
+// blocks come in rows (whole rounds of the XCDs); those behind the last do
+// nothing.
+constexpr unsigned kGridRow = 1u << 23;
+inline dim3 grid_of(unsigned blocks) {
+  if (blocks <= kGridRow) return dim3(blocks);
+  return dim3(kGridRow, (blocks + kGridRow - 1) / kGridRow);
+}
+__device__ __forceinline__ uint32_t block_number() {
+  return blockIdx.y * gridDim.x + blockIdx.x;
+}
+
 // The block's columns and part.  Without clouds in runs for each XCD (as
 // xcd_block), the parts of a tile after each other.  In a batch the tiles' work
 // is their clouds': the XCDs come in groups of `stripe`, each group has some of
@@ -509,18 +521,20 @@ constexpr int kFewUnits = 32;  // in order: some XCDs would have none
 __device__ __forceinline__ bool unit_of(const Attn &a, int32_t &tile,
                                         int32_t &kvh, int32_t &split) {
   const int32_t units = a.tiles * a.kv_heads;
+  const uint32_t block = block_number();
+  const int32_t x = (int32_t)(block % kXcd), j = (int32_t)(block / kXcd);
   int32_t u;
   if (!a.q_off) {
-    const int32_t b = xcd_block();
+    const int32_t per = (units * a.splits + kXcd - 1) / kXcd;
+    if (j >= per) return false;
+    const int32_t b = x * per + j;
     u = b / a.splits;
     split = b % a.splits;
   } else if (units < kFewUnits) {
-    u = (int32_t)blockIdx.x % units;
-    split = (int32_t)blockIdx.x / units;
+    u = (int32_t)block % units;
+    split = (int32_t)block / units;
   } else {
     const int32_t per = (units + kXcd - 1) / kXcd;
-    const int32_t x = (int32_t)(blockIdx.x % kXcd);
-    const int32_t j = (int32_t)(blockIdx.x / kXcd);
     split = j / per;
     const int32_t each = units / (kXcd / a.stripe);
     const int32_t v = j % per * a.stripe + x % a.stripe;
@@ -941,21 +955,26 @@ __device__ __forceinline__ float delta_of(const T *dout, const T *out, int g,
 }
 
 // D of every row and head, four lanes each, where k_attn_dq does not run.
+constexpr int64_t kDeltaGrid = (int64_t)1 << 20;  // blocks of its launch
 template <class T, int B>
 __global__ __launch_bounds__(kAttnNT) void k_attn_delta(Attn a) {
+  constexpr int kPer = kAttnNT / 4;
   const int64_t cols = (int64_t)a.nq * a.heads;
-  const int64_t at = ((int64_t)blockIdx.x * kAttnNT + threadIdx.x) / 4;
-  const int64_t c = min(at, cols - 1);
-  const int64_t row = c / a.heads;
-  const int32_t head = (int32_t)(c % a.heads);
-  float sum = delta_of<T, B>(
-      static_cast<const T *>(a.dout) + row * a.lddo + (int64_t)head * a.dh,
-      static_cast<const T *>(a.out) + row * a.ldo + (int64_t)head * a.dh,
-      threadIdx.x % 4, a.dh);
-  sum += __shfl_xor(sum, 1, kWave);
-  sum += __shfl_xor(sum, 2, kWave);
-  if (threadIdx.x % 4 == 0 && at < cols)
-    a.delta[(int64_t)head * a.nq + row] = sum;
+  for (int64_t c0 = (int64_t)blockIdx.x * kPer; c0 < cols;
+       c0 += (int64_t)gridDim.x * kPer) {
+    const int64_t at = c0 + threadIdx.x / 4;
+    const int64_t c = min(at, cols - 1);
+    const int64_t row = c / a.heads;
+    const int32_t head = (int32_t)(c % a.heads);
+    float sum = delta_of<T, B>(
+        static_cast<const T *>(a.dout) + row * a.lddo + (int64_t)head * a.dh,
+        static_cast<const T *>(a.out) + row * a.ldo + (int64_t)head * a.dh,
+        threadIdx.x % 4, a.dh);
+    sum += __shfl_xor(sum, 1, kWave);
+    sum += __shfl_xor(sum, 2, kWave);
+    if (threadIdx.x % 4 == 0 && at < cols)
+      a.delta[(int64_t)head * a.nq + row] = sum;
+  }
 }
 
 // lse of a row in base 2, +inf where it has no keys: P is 0 there

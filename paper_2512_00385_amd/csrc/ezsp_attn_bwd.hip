@@ -13,7 +13,7 @@ void dq(Attn g, hipStream_t st) {
   plan_parts<T>(g, cols, kCols, g.nk, R,
                 (int64_t)g.nq * g.heads * width_of(B));
   hipLaunchKernelGGL((k_attn_dq<T, B, NC, R>),
-                     dim3(attn_grid(g)), dim3(kAttnNT), 0, st, g);
+                     grid_of(attn_grid(g)), dim3(kAttnNT), 0, st, g);
   if (g.splits > 1) {
     constexpr int D = width_of(B);
     const int64_t lanes = (int64_t)g.nq * g.heads * (D / 4);
@@ -31,7 +31,7 @@ void dkv(Attn g, hipStream_t st) {
   plan_parts<T>(g, g.nk, kCols, (int64_t)g.nq * g.group, R,
                 (int64_t)g.nk * g.kv_heads * 2 * width_of(B));
   hipLaunchKernelGGL((k_attn_dkv<T, B, NC, R, KEPT>),
-                     dim3(attn_grid(g)), dim3(kAttnNT), 0, st, g);
+                     grid_of(attn_grid(g)), dim3(kAttnNT), 0, st, g);
   if (g.splits > 1) {
     constexpr int D = width_of(B);
     const int64_t lanes = (int64_t)g.nk * g.kv_heads * (D / 4);
@@ -66,7 +66,8 @@ void both(const Attn &g, hipStream_t st) {
   } else {
     const int64_t lanes = (int64_t)g.nq * g.heads * 4;
     hipLaunchKernelGGL((k_attn_delta<T, B>),
-                       dim3((unsigned)((lanes + kAttnNT - 1) / kAttnNT)),
+                       dim3((unsigned)std::min(
+                           (lanes + kAttnNT - 1) / kAttnNT, kDeltaGrid)),
                        dim3(kAttnNT), 0, st, g);
   }
   if (!g.dk && !g.dv) return;

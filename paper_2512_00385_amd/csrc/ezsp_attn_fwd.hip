@@ -14,7 +14,7 @@ void launch(Attn g, hipStream_t st) {
   plan_parts<T>(g, cols, kCols, g.nk, R,
                 (int64_t)g.nq * g.heads * (width_of(B) + 2));
   hipLaunchKernelGGL((k_attn_fwd<T, B, NC, R>),
-                     dim3(attn_grid(g)), dim3(kAttnNT), 0, st, g);
+                     grid_of(attn_grid(g)), dim3(kAttnNT), 0, st, g);
   if (g.splits == 1) return;
   constexpr int D = width_of(B), kPer = kAttnNT / (D / 4);
   const int64_t joined = (int64_t)g.nq * g.heads;
