@@ -653,6 +653,22 @@ __device__ __forceinline__ float lanes16_sum(float v) {
 
 // --- forward -----------------------------------------------------------------
 
+// Groups of 16 columns a wave and keys a tile: as the registers of two waves a
+// SIMD hold, of three with short heads, whose exponentials are the work
+// (1,265,474 x 613, 4 heads of 32: 3 groups of columns 755 us, 4 840, 2 782;
+// 100,000 x 2000, 8 of 64: 4 groups 494, 3 510).  With few columns, unless
+// parts of their keys fill the chip, one group (of wide heads with tiles that
+// leave LDS for three blocks a CU: 64 rows to 2000 keys each, 8 heads of 128:
+// 127 us with tiles of 32, 166 with 64).
+template <class T, int B>
+struct ForwardShape {
+  static constexpr bool kBf = sizeof(T) == 2;
+  static constexpr int kGroups =
+      kBf ? (B <= 3 ? 3 : B == 4 ? 4 : 2) : (B <= 4 ? 2 : 1);
+  static constexpr int kKeys = B <= 2 || (kBf && B > 4) ? 64 : 32;
+  static constexpr int kFewKeys = B <= 2 || (kBf && B <= 4) ? 64 : 32;
+};
+
 constexpr float kGrown = 4096.0f;
 
 // P = 2^(S c - mc) of a lane's scores as operands, and its sum over them
@@ -935,6 +951,22 @@ __global__ __launch_bounds__(kAttnNT) void k_attn_join(Attn a) {
 }
 
 // --- backward ----------------------------------------------------------------
+
+// Groups of 16 columns a wave: as the registers of two waves a SIMD hold, half
+// of them where the blocks would leave CUs idle, in parts too.  Keys a tile for
+// dq, rows a tile for dk and dv: the rows of q that pass a key block come from
+// further away than keys, longer tiles cover their latency.  (100,000 x 2000, 8
+// heads of 64: 2253 us with tiles of 32 rows, 2020 of 64, 1949 of 128;
+// 1,265,474 x 613, 4 of 32: 3158 of 64, 2730 of 128; fp32, 200,000 x 1000, 4 of
+// 32: 3737 and 3609.)  kKept: k_attn_dkv's v in LDS.
+template <class T, int B>
+struct BackwardShape {
+  static constexpr bool kBf = sizeof(T) == 2;
+  static constexpr int kGroups = kBf || B <= 4 ? 2 : 1;
+  static constexpr int kKeys = B <= 2 ? 64 : 32;
+  static constexpr int kRows = B <= 2 || (kBf && B <= 4) ? 128 : 32;
+  static constexpr bool kKept = kBf && B > 4;
+};
 
 // What lane group g has of D = dout . out of a row and head.  Both kernels
 // that need it add in this order and then over the groups, g ^ 1 first.

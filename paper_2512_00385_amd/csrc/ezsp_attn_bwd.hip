@@ -43,16 +43,8 @@ void dkv(Attn g, hipStream_t st) {
 
 template <class T, int B>
 void both(const Attn &g, hipStream_t st) {
-  // columns a wave and tile: as the registers of two waves a SIMD hold, half
-  // of them where the blocks would leave CUs idle, in parts too
-  constexpr bool kBf = sizeof(T) == 2;
-  constexpr int R = B <= 2 ? 64 : 32;
-  // (the rows of q that pass a key block come from further away than keys:
-  // longer tiles cover their latency.  100,000 x 2000, 8 heads of 64: 2253 us
-  // with tiles of 32 rows, 2020 of 64, 1949 of 128; 1,265,474 x 613, 4 of 32:
-  // 3158 of 64, 2730 of 128; fp32, 200,000 x 1000, 4 of 32: 3737 and 3609)
-  constexpr int RQ = B <= 2 || (kBf && B <= 4) ? 128 : 32;
-  constexpr int N = kBf || B <= 4 ? 2 : 1;
+  typedef BackwardShape<T, B> S;
+  constexpr int N = S::kGroups, R = S::kKeys, RQ = S::kRows;
   auto few = [&](int64_t cols, int64_t lines) {
     const int64_t per = kAttnWaves * 16 * 2;
     return (cols + per - 1) / per * g.kv_heads < kCus &&
@@ -74,7 +66,7 @@ void both(const Attn &g, hipStream_t st) {
   if (few(g.nk, (int64_t)g.nq * g.group))
     dkv<T, B, 1, RQ, false>(g, st);
   else
-    dkv<T, B, N, RQ, kBf && (B > 4)>(g, st);
+    dkv<T, B, N, RQ, S::kKept>(g, st);
 }
 
 template <class T>

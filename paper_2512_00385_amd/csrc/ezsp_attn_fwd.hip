@@ -29,23 +29,14 @@ void launch(Attn g, hipStream_t st) {
 
 template <class T, int B>
 void by_columns(const Attn &g, hipStream_t st) {
-  // columns a wave and tile: as the registers of two waves a SIMD hold, of
-  // three with short heads, whose exponentials are the work (1,265,474 x 613,
-  // 4 heads of 32: 3 groups of columns 755 us, 4 840, 2 782; 100,000 x 2000, 8
-  // of 64: 4 groups 494, 3 510)
-  constexpr bool kBf = sizeof(T) == 2;
-  constexpr int N = kBf ? (B <= 3 ? 3 : B == 4 ? 4 : 2) : (B <= 4 ? 2 : 1);
-  constexpr int R = B <= 2 || (kBf && B > 4) ? 64 : 32;
-  // with few columns, unless parts of their keys fill the chip, waves of 16 (of
-  // wide heads with tiles that leave LDS for three blocks a CU: 64 rows to 2000
-  // keys each, 8 heads of 128: 127 us with tiles of 32, 166 with 64)
-  constexpr int kFewR = B <= 2 || (kBf && B <= 4) ? 64 : 32;
+  typedef ForwardShape<T, B> S;
+  constexpr int N = S::kGroups;
   const int64_t cols = (int64_t)g.nq * g.group * g.kv_heads;
   if (cols < 256 * kAttnWaves * 16 &&
       !parts_fill<T>(g, (int64_t)g.nq * g.group, kAttnWaves * 16 * N, g.nk))
-    launch<T, B, 1, kFewR>(g, st);
+    launch<T, B, 1, S::kFewKeys>(g, st);
   else
-    launch<T, B, N, R>(g, st);
+    launch<T, B, N, S::kKeys>(g, st);
 }
 
 template <class T>
