@@ -342,6 +342,7 @@ inline Attn attn_of(const AttnArgs &a) {
 
 constexpr int kMaxSplits = 64;  // a lane of the join each
 constexpr int64_t kPartFloats = (int64_t)64 << 20;  // of the parts' sums
+constexpr int64_t kLeastLines = 32;                 // of a part: a tile's
 constexpr int64_t kCus = 256;                       // of an MI355X
 
 // The parts of a call's lines: `cols` columns of each head of k in blocks of
@@ -359,7 +360,8 @@ constexpr int64_t kCus = 256;                       // of an MI355X
 // more of them, up to twice a mean one's.  (Backward of 16,384 x 12,288 in
 // eight clouds of one to six lengths, 16 heads of 128 on 4: 994 us, 1242 with
 // each cloud whole; 20,011 x 3511 in eleven, 6 heads of 40 in fp32: 360 and
-// 475.  With up to four times a mean one's nothing changes.)
+// 475.  With up to four times a mean one's nothing changes.)  attn_reserve
+// counts with at most 2 lines / kLeastLines parts.
 template <class T>
 void plan_parts(Attn &g, int64_t cols, int64_t per, int64_t lines,
                 int64_t least, int64_t floats) {

@@ -10,6 +10,7 @@ void dq(Attn g, hipStream_t st) {
   const int64_t cols = (int64_t)g.nq * g.group;
   g.tiles = (int32_t)(g.q_off ? cols / kCols + g.clouds
                               : (cols + kCols - 1) / kCols);
+  static_assert(R >= kLeastLines, "as attn_reserve counts");
   plan_parts<T>(g, cols, kCols, g.nk, R,
                 (int64_t)g.nq * g.heads * width_of(B));
   hipLaunchKernelGGL((k_attn_dq<T, B, NC, R>),
@@ -28,6 +29,7 @@ void dkv(Attn g, hipStream_t st) {
   constexpr int kCols = kAttnWaves * 16 * NC;
   g.tiles = (int32_t)(g.k_off ? g.nk / kCols + g.clouds
                               : (g.nk + kCols - 1) / kCols);
+  static_assert(R >= kLeastLines, "as attn_reserve counts");
   plan_parts<T>(g, g.nk, kCols, (int64_t)g.nq * g.group, R,
                 (int64_t)g.nk * g.kv_heads * 2 * width_of(B));
   hipLaunchKernelGGL((k_attn_dkv<T, B, NC, R, KEPT>),

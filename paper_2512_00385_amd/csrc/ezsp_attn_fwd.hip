@@ -11,6 +11,7 @@ void launch(Attn g, hipStream_t st) {
   g.tiles = (int32_t)(g.q_off ? cols / kCols + g.clouds
                               : (cols + kCols - 1) / kCols);
   // few columns leave the chip empty: the keys in parts of two tiles or more
+  static_assert(R >= kLeastLines, "as attn_reserve counts");
   plan_parts<T>(g, cols, kCols, g.nk, R,
                 (int64_t)g.nq * g.heads * (width_of(B) + 2));
   hipLaunchKernelGGL((k_attn_fwd<T, B, NC, R>),
@@ -55,18 +56,24 @@ void dispatch(const Attn &g, hipStream_t st) {
 void attn_reserve(Arena &ar, int64_t nq, int64_t nk, int64_t heads,
                   int64_t kv_heads, int64_t dh, bool bwd, AttnArgs *a) {
   const int64_t d = width_of((int)((dh + 15) / 16));
-  // kMaxSplits parts of the sums, or as many as come to kPartFloats
-  auto floats = [](int64_t part) {
-    return std::min<int64_t>(part * kMaxSplits, kPartFloats);
+  // As many parts of the sums as plan_parts may choose, up to kPartFloats; a
+  // size that grows with every argument.  (Calls of so many columns that they
+  // come in one part have kPartFloats too, as smaller ones use it.)
+  const auto floats = [](int64_t part, int64_t parts) {
+    return (size_t)std::min(part * parts, kPartFloats);
   };
+  const int64_t of_keys = std::min<int64_t>(kMaxSplits, 2 * (nk / kLeastLines));
   if (!bwd) {
-    a->part = ar.take<float>((size_t)floats(nq * heads * (d + 2)));
+    a->part = ar.take<float>(floats(nq * heads * (d + 2), of_keys));
     return;
   }
   a->delta = ar.take<float>((size_t)(nq * heads));
-  // (dq's and then dk's and dv's)
-  a->part = ar.take<float>((size_t)std::max(floats(nq * heads * d),
-                                            floats(nk * kv_heads * 2 * d)));
+  // dq's and then dk's and dv's, whose lines are the rows of heads / kv_heads
+  // heads: the parts of all kv_heads
+  const int64_t of_rows = std::min<int64_t>(kMaxSplits * kv_heads,
+                                            2 * nq * heads / kLeastLines);
+  a->part = ar.take<float>(std::max(floats(nq * heads * d, of_keys),
+                                    floats(nk * 2 * d, of_rows)));
 }
 
 int attn_fwd_run(const AttnArgs &a, hipStream_t st) {

@@ -1,8 +1,8 @@
 // attn_plan.cpp -- what cross attention launches, over the sizes that its
 // entry points take: the launches are recorded, not run.  Each keeps to what a
 // launch may have (below 2^32 threads along x, below 2^16 blocks along y), has
-// a block for every unit of its work, and every block its own.  Prints a line
-// per check; exits 1 if one fails.
+// a block for every unit of its work, and every block its own; the workspace
+// holds the sums of its parts.  Prints a line per check; exits 1 if one fails.
 #include "lanes.h"
 
 #include <stdio.h>
@@ -104,6 +104,38 @@ void check_launches(const Call &c) {
   }
 }
 
+size_t reserved(const Call &c, bool backward) {
+  Arena ar;
+  AttnArgs a = {};
+  attn_reserve(ar, c.nq, c.nk, c.heads, c.kv_heads, c.dh, backward, &a);
+  return ar.off;
+}
+// what a call's parts and D take is there; and a call with too few keys and
+// rows for parts asks for D alone (a piece's alignment apart)
+void check_workspace(const Call &c) {
+  const size_t forward = reserved(c, false), backward = reserved(c, true);
+  const size_t delta = (size_t)c.nq * c.heads * sizeof(float);
+  call(c);
+  for (const Launch &l : launches) {
+    if (l.a.splits == 1) continue;
+    const size_t d = width_of((c.dh + 15) / 16), splits = l.a.splits;
+    if (is(l, "k_attn_fwd"))
+      check(splits * c.nq * c.heads * (d + 2) * sizeof(float) <= forward,
+            "forward workspace too small", l);
+    if (is(l, "k_attn_dq"))
+      check(delta + splits * c.nq * c.heads * d * sizeof(float) <= backward,
+            "dq workspace too small", l);
+    if (is(l, "k_attn_dkv"))
+      check(delta + splits * c.nk * c.kv_heads * 2 * d * sizeof(float) <=
+                backward,
+            "dk, dv workspace too small", l);
+  }
+  if (c.nk < 32)
+    check(forward == 0, "workspace without parts", launches[0]);
+  if (c.nk < 32 && c.nq * c.heads < 16)
+    check(backward <= delta + 256, "workspace without parts", launches[0]);
+}
+
 // Every tile, head and part has one block, in rows of `row` blocks.
 bool each_once(int32_t tiles, int32_t kv_heads, int32_t splits, bool batch,
                unsigned row) {
@@ -169,6 +201,13 @@ int main() {
   }
   for (const Call &c : calls) check_launches(c);
   printf("launches of %zu calls: %s\n", calls.size(), ok ? "fit" : "do not fit");
+  const bool fit = ok;
+  ok = true;
+  calls.push_back({70001, 3, 2, 2, 16, 0, 0});
+  calls.push_back({7, 31, 2, 1, 128, 1, 0});
+  for (const Call &c : calls) check_workspace(c);
+  const bool held = ok;
+  printf("workspaces: %s\n", held ? "fit" : "do not fit");
 
   bool once = true;
   for (bool batch : {false, true})
@@ -178,5 +217,5 @@ int main() {
           for (unsigned row : {64u, 1024u, kGridRow})
             once &= each_once(tiles, heads, splits, batch, row);
   printf("units: %s\n", once ? "one block each" : "wrong");
-  return ok && once ? 0 : 1;
+  return fit && held && once ? 0 : 1;
 }

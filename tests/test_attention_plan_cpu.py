@@ -1,10 +1,12 @@
 """What cross attention launches, on the CPU from its own source: the launches
 are recorded (cpu_lanes/attn_plan.cpp), from the smallest sizes to the largest
-that the entry points take."""
+that the entry points take; and the workspaces that hold their parts."""
 import os
 import subprocess
 
 import pytest
+
+from paper_2512_00385_amd import ezsp
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CLANG = "/opt/rocm/llvm/bin/clang++"  # the kernels' vector types are clang's
@@ -34,3 +36,19 @@ def test_launches_fit(lines):
 
 def test_every_unit_has_one_block(lines):
     assert "units: one block each" in lines
+
+
+def test_workspaces_hold_the_parts(lines):
+    """And calls that cannot come in parts ask for no sums of these."""
+    assert "workspaces: fit" in lines, "\n".join(lines[:20])
+
+
+@pytest.mark.skipif(not os.path.exists(ezsp.LIB_PATH),
+                    reason="libezsp.so not built")
+def test_workspace_of_few_keys():
+    """70,001 rows to 3 keys come in one part forward; backward 64 of the
+    keys' sums and D."""
+    lib = ezsp.load()
+    assert lib.ezsp_cross_attention_workspace_size(70_001, 3, 2, 2, 16) < 4096
+    assert lib.ezsp_cross_attention_backward_workspace_size(
+        70_001, 3, 2, 2, 16) < 4 * (70_001 * 2 + 64 * 3 * 2 * 64) + 4096
