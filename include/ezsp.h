@@ -543,7 +543,8 @@ size_t ezsp_log_probs_workspace_size(int64_t n, int32_t v, int32_t top);
  *             Scores of -inf are not given: such places hold -1 and -inf
  * A row whose scores are all -inf has no probabilities: lse, and logp of a
  * class, are -inf, entropy is 0.  NaN or +inf among the scores make a row's
- * lse, logp, entropy and top_logp NaN.
+ * lse, logp and entropy NaN, and top_logp of the classes given, of which one
+ * with a score of NaN is none.
  * Errors: INVALID_ARG, WORKSPACE, DEVICE. */
 int ezsp_log_probs(const void *x, int64_t ldx, int32_t type, int64_t n,
                    int32_t v, const int32_t *ids, float *logp, float *lse,
@@ -557,7 +558,8 @@ int ezsp_log_probs(const void *x, int64_t ldx, int32_t type, int64_t n,
  *             none of it
  *   ids       n int32 (in; NULL with dlogp NULL)
  *   lse       n fp32 (in): as ezsp_log_probs gave it (rounded to fp32, which
- *             puts p off by |lse| 2^-24 of itself)
+ *             puts p off by |lse| 2^-24 of itself; its own exponential by 3
+ *             |x_j - lse| 2^-24 and 2^-22)
  *   entropy, dentropy  n fp32 (in, both or neither)
  *   dx        n rows of v, type (out); may be x
  * A row whose scores are all -inf has dx = 0, as has every score of -inf
@@ -601,8 +603,9 @@ size_t ezsp_cross_attention_workspace_size(int64_t nq, int64_t nk,
  *           without keys
  * S, its exponentials and every sum are fp32; with bfloat16, exp(S - m), m
  * the largest S met so far, is rounded to bfloat16 for the product with v,
- * the matrix cores' input.  (S of 2^24 and more leaves fp32 no digits for its
- * exponential; a key with S below -10^30 scale is as good as masked.)
+ * the matrix cores' input.  (An exponential of S is off by some 3 |S| 2^-24 of
+ * itself, backward also by some 3 |lse| 2^-24; S of 2^24 and more leaves fp32
+ * no digits for it.  A key with S below -10^30 scale is as good as masked.)
  * Errors: INVALID_ARG, WORKSPACE, DEVICE. */
 int ezsp_cross_attention(const void *q, int64_t ldq, int64_t nq,
                          const void *k, int64_t ldk, const void *v,

@@ -1138,7 +1138,8 @@ def cross_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
     128; kv_heads is heads by default, else a divisor of it.  q_offsets and
     k_offsets [clouds + 1] int32, on the device, confine the rows of each
     cloud to its own keys; key_bias [nk] fp32 is added to the scores of each
-    key, -inf masks it; scale is d ** -0.5 by default.  Returns out
+    key, -inf masks it, and has no gradient; scale, from 2^-16 to 2^16, is
+    d ** -0.5 by default.  Returns out
     [nq, heads * d], 0 for a row without keys, or with want_lse (out, lse
     [heads, nq] fp32) for cross_attention_backward, which is where gradients
     come from: torch's own differentiation stops here.  Computed in stream
