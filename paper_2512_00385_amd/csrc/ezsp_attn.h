@@ -25,14 +25,16 @@
 // What bounds them, measured on one MI355X.  Short heads in bfloat16: vector
 // instructions, since each score takes an exponential (a quarter of the rate),
 // a fused product, an addition and half a conversion (forward of 1,265,474 x
-// 613, 4 heads of 32: 736 us, vector instructions issue in 0.8 of the cycles,
-// the matrix cores are busy in 0.24).  Long heads: the matrix cores, at 0.7 of
-// a large library product's rate where rows and keys are many (400,000 x 3000:
-// heads of 128 and 64 at 890 TFLOP/s; gradients 820 to 1000), less where
+// 613, 4 heads of 32: 1.75 million cycles, in 0.79 of them vector instructions
+// issue, in 0.24 the matrix cores are busy; 736 us at the full clock, 870 at
+// that of a chip that has rested).  Long heads: the matrix cores, at 0.7 of a
+// large library product's rate where rows and keys are many (400,000 x 3000:
+// heads of 128 and 64 at 890 to 920 TFLOP/s; gradients 820 to 1040), less where
 // clouds are small and uneven.  fp32: its matrix instructions (busy in 0.63 to
 // 0.69 of the cycles in gradients of 20,011 x 3511 in eleven clouds).  One row:
-// the keys' bytes and two launches (8192 keys, 32 heads on 8 of 128: 16 us, 13
-// and 4 in the kernels).
+// latency (8192 keys, 32 heads on 8 of 128: 16 us, 13 and 4 in the kernels, 2.5
+// TB/s: one of a block's waves has columns, and its two tiles of keys come one
+// after the other).
 #pragma once
 
 #include <math.h>
@@ -159,14 +161,18 @@ __device__ __forceinline__ void store4(float *p, f32x4_t v, int cnt) {
   }
 }
 
-// Lines of D elements, a power of two, in LDS.  16 lines read along, or four
-// groups of four read across, are to meet each bank as often as they must (16
-// pieces of 16 bytes are all banks once).  Lines of 256 bytes and more lie an
-// odd number of pieces apart; the pieces of shorter ones, which would then
-// meet when they are written, are exchanged by the line's number.  (Exchanged,
-// the pieces of long lines took two dozen registers for their addresses,
-// which are offsets of one otherwise: backward of 128 bfloat16 2084 us for
-// 2386, of 32 the other way round 2365 for 2391.)
+// Lines of D elements, a power of two, in LDS, placed so that 16 lines read
+// along, or four groups of four read across, have all banks once (16 pieces of
+// 16 bytes).  Lines of 256 bytes and more lie an odd number of pieces apart, the
+// pieces of shorter ones are exchanged by the line's number.  (Exchanged, the
+// pieces of long lines took two dozen registers for their addresses, which are
+// offsets of one otherwise: backward of 16,384 x 12,288 in eight clouds, 16
+// heads of 128 on 4: 970 us, 1066 exchanged.  Short lines apart: nothing,
+// 1,265,474 x 613, 4 of 32 2282 us and 2271.)  What the banks make of it, in
+// short kernels of one access each, against the 4 cycles of an instruction of
+// 64 pieces in a row: bfloat16 across and put meet none twice, along takes 8 in
+// every layout, so its lanes are not served 16 in turn; fp32 across takes the
+// least (half as much again for lines of 32 elements), along and put twice it.
 template <class T, int D>
 struct Lines {
   static constexpr int kPieces = D * (int)sizeof(T) / 16;
@@ -358,9 +364,10 @@ constexpr int64_t kCus = 256;                       // of an MI355X
 // bfloat16 needs two blocks a CU for its full speed, fp32, bound by its matrix
 // instructions, one.  A batch's parts have one length, so that a long cloud has
 // more of them, up to twice a mean one's.  (Backward of 16,384 x 12,288 in
-// eight clouds of one to six lengths, 16 heads of 128 on 4: 994 us, 1242 with
-// each cloud whole; 20,011 x 3511 in eleven, 6 heads of 40 in fp32: 360 and
-// 475.  With up to four times a mean one's nothing changes.)  attn_reserve
+// eight clouds of one to six lengths, 16 heads of 128 on 4, three drawings: 966,
+// 1058 and 1017 us, 1172, 1342 and 1344 with each cloud whole; 20,011 x 3511 in
+// eleven, 6 heads of 40 in fp32: 346, 338 and 344, and 446, 508 and 516.  With
+// up to four times a mean one's nothing changes.)  attn_reserve
 // counts with at most 2 lines / kLeastLines parts.
 template <class T>
 void plan_parts(Attn &g, int64_t cols, int64_t per, int64_t lines,
@@ -402,11 +409,12 @@ void plan_parts(Attn &g, int64_t cols, int64_t per, int64_t lines,
 // a sixteenth of such a block's columns beyond those of halves of it; not for
 // batches in fp32, whose clouds end in half empty blocks of more matrix
 // instructions.  (Gradients of keys, by waves of 16 and of 32 columns:
-// 1,265,474 x 613, 4 heads of 32: 2067 and 1528 us; 400,000 x 3000, 8 of 128:
-// 17.5 and 11.7 ms; 20,000 x 613, 8 of 64: 112 and 95; of 100 keys, 256 blocks
-// with parts: 568 and 603; fp32, 100,000 x 2000, 8 of 64: 10.4 and 7.7 ms;
-// 100,000 x 2400 in eight clouds, 8 of 48: 925 and 1234.  2000 rows to 100,000
-// keys each, 8 heads of 64: forward 962 and 590, dq 1077 and 748.)
+// 1,265,474 x 613, 4 heads of 32: 2014 and 1418 us; 400,000 x 3000, 8 of 128:
+// 17.5 and 11.8 ms; 20,000 x 613, 8 of 64: 111 and 90; 100,000 x 100, 8 of 64:
+// 141 and 130; of 100 keys, 256 blocks with parts: 568 and 603; fp32, 100,000 x
+// 2000, 8 of 64: 10.3 and 7.7 ms; 100,000 x 2400 in eight clouds, 8 of 48: 956
+// and 1220.  2000 rows to 100,000 keys each, 8 heads of 64: forward 910 and 507,
+// dq 1064 and 722.)
 template <class T>
 bool parts_fill(const Attn &g, int64_t cols, int64_t wide, int64_t lines) {
   if (g.q_off && sizeof(T) == 4) return false;
@@ -514,8 +522,9 @@ __device__ __forceinline__ uint32_t block_number() {
 // is their clouds': the XCDs come in groups of `stripe`, each group has some of
 // the heads whole, and its XCDs take their tiles in turn, so that each has its
 // share of every cloud and a head's lines pass through few L2s (backward of
-// 16,384 x 12,288 in eight clouds, 16 heads of 128 on 4: 1025 us, 1121 in runs,
-// 1075 with all tiles in turn over all XCDs).  And all tiles have their first
+// 16,384 x 12,288 in eight clouds, 16 heads of 128 on 4, three drawings: 966,
+// 1058 and 1017 us, in runs 971, 1107 and 1062, with all tiles in turn over all
+// XCDs 1005, 1083 and 1079).  And all tiles have their first
 // part before any has its second, so that the parts which a cloud has not end
 // together: in a row they fell on the same CUs each time and left the work to
 // the others (dq of 20,011 x 3511 in eleven clouds, two of them in two parts of
@@ -657,11 +666,12 @@ __device__ __forceinline__ float lanes16_sum(float v) {
 
 // Groups of 16 columns a wave and keys a tile: as the registers of two waves a
 // SIMD hold, of three with short heads, whose exponentials are the work
-// (1,265,474 x 613, 4 heads of 32: 3 groups of columns 755 us, 4 840, 2 782;
-// 100,000 x 2000, 8 of 64: 4 groups 494, 3 510).  With few columns, unless
-// parts of their keys fill the chip, one group (of wide heads with tiles that
-// leave LDS for three blocks a CU: 64 rows to 2000 keys each, 8 heads of 128:
-// 127 us with tiles of 32, 166 with 64).
+// (1,265,474 x 613 with a bias, 4 heads of 32: 3 groups of columns 765 us, 4
+// 831, 2 780, without one 722, 764 and 706; 400,000 x 3000, 8 of 32: 1817, 1932
+// and 1863; 100,000 x 2000, 8 of 48: 451, 493 and 462; of 64: 4 groups 501, 3
+// 555).  With few columns, unless parts of their keys fill the chip, one group
+// (of wide heads with tiles that leave LDS for three blocks a CU: 64 rows to
+// 2000 keys each, 8 heads of 128: 105 us with tiles of 32, 113 with 64).
 template <class T, int B>
 struct ForwardShape {
   static constexpr bool kBf = sizeof(T) == 2;
@@ -957,10 +967,10 @@ __global__ __launch_bounds__(kAttnNT) void k_attn_join(Attn a) {
 // Groups of 16 columns a wave: as the registers of two waves a SIMD hold, half
 // of them where the blocks would leave CUs idle, in parts too.  Keys a tile for
 // dq, rows a tile for dk and dv: the rows of q that pass a key block come from
-// further away than keys, longer tiles cover their latency.  (100,000 x 2000, 8
-// heads of 64: 2253 us with tiles of 32 rows, 2020 of 64, 1949 of 128;
-// 1,265,474 x 613, 4 of 32: 3158 of 64, 2730 of 128; fp32, 200,000 x 1000, 4 of
-// 32: 3737 and 3609.)  kKept: k_attn_dkv's v in LDS.
+// further away than keys, longer tiles cover their latency.  (Backward of
+// 100,000 x 2000, 8 heads of 64: 1573 us with tiles of 64 rows, 1545 of 128;
+// 1,265,474 x 613, 4 of 32: 2361 and 2282; fp32, 200,000 x 1000, 4 of 32: 3329
+// and 3249.)  kKept: k_attn_dkv's v in LDS.
 template <class T, int B>
 struct BackwardShape {
   static constexpr bool kBf = sizeof(T) == 2;
@@ -1328,7 +1338,8 @@ __global__ __launch_bounds__(kAttnNT, W) void k_attn_dkv(Attn a) {
       }
       // the lines for the products that follow are read behind the scores, not
       // among them, whose registers they would take (16,384 x 12,288 in
-      // eight clouds, 16 heads of 128 on 4: 988 us, 1019 without this)
+      // eight clouds, 16 heads of 128 on 4, three drawings: 966, 1058 and 1017
+      // us, 997, 1094 and 1055 without this)
       __builtin_amdgcn_sched_barrier(0);
       frag_t<T> p[NC], ds[NC];
 #pragma unroll

@@ -651,11 +651,18 @@ constexpr int64_t kCus = 256;  // of an MI355X
 bool many_rows(int64_t n) { return n >= 2 * kCus; }
 
 // Parts of a long row: as many as give every CU a block, each of at least 8K
-// scores (one row of 40,000 with eight classes: 13.4 us, 16.9 in parts of 16K;
-// of 300,000 16.2 and 18.2), but no more than eight while these stay below 24K:
-// the join sorts up to 64 scores of all parts at once (131,072 with eight
-// classes: 13.0 us in eight parts, 16.1 in sixteen), and not two, for which the
-// second launch takes longer than they save (20,000: 12.5 us whole, 13.4).
+// scores (one row of 40,000 with eight classes: 13.3 us, 16.8 whole; of 300,000
+// 16.2, in parts of 16K 18.2), but no more than eight while these stay below
+// 24K: the join sorts up to 64 scores of all parts at once (131,072 with eight
+// classes: 12.9 us in eight parts, 15.7 in sixteen), and not two, for which the
+// second launch takes longer than they save (20,000: 12.7 us whole, 13.4).  The
+// rule was set with eight classes and does not read their number.  With none to
+// four, which the join would sort from more parts, it is within 0.6 us of the
+// best of 1, 4, 8, 16 and 24 parts up to 131,072 scores; at 196,608, the last row
+// of eight parts, sixteen are sooner (none 7.9 us and 9.6, four 12.7 and 16.5,
+// eight 15.7 and 17.3); and with more than eight the join takes them one after
+// the other, so that few or no parts are sooner (65,536 with sixteen: 13.3 us in
+// four, 19.8; 40,000 with 32: 17.9 whole, 27.3).
 int32_t parts_of(int64_t n, int32_t v) {
   int64_t most = std::min<int64_t>(kMaxParts, v / 8192);
   if (most > 8 && v / 8 <= 24576) most = 8;
